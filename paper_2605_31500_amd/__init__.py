@@ -31,11 +31,19 @@ EXPORTED_SYMBOLS = (
     "gt_workspace_pool_stats",
 )
 
+# the entry points of include/gt_layer.h
+LAYER_SYMBOLS = ("gt_diff_attn_fwd", "gt_diff_attn_bwd", "gt_rope", "gt_layernorm_fwd", "gt_layernorm_bwd")
+
 
 class GtTuning(ctypes.Structure):
     _fields_ = [("light_max_deg", ctypes.c_int32), ("heavy_min_deg", ctypes.c_int32),
                 ("chunk_edges", ctypes.c_int32), ("grid_blocks", ctypes.c_int32),
                 ("dense_tiles", ctypes.c_int32), ("bf16_weights", ctypes.c_int32)]
+
+
+class GtRopeSpec(ctypes.Structure):
+    _fields_ = [("axes", ctypes.c_int32), ("dims", ctypes.c_int32 * 4), ("layout", ctypes.c_int32),
+                ("theta", ctypes.c_double)]
 
 
 class GtError(RuntimeError):
@@ -79,6 +87,13 @@ def load_library(path: str = LIB_PATH):
     L.gt_profile_collect.argtypes = [ctypes.POINTER(ctypes.c_double), ctypes.POINTER(i64)]
     L.gt_workspace_release.argtypes = []
     L.gt_workspace_pool_stats.argtypes = [i32, ctypes.POINTER(ctypes.c_uint64), ctypes.POINTER(ctypes.c_uint64)]
+    L.gt_diff_attn_fwd.argtypes = [ctypes.c_int] + [P] * 8 + [i64, i64, i32, i32, f32, ctypes.POINTER(GtTuning), P]
+    L.gt_diff_attn_bwd.argtypes = [ctypes.c_int] + [P] * 14 + [i64, i64, i32, i32, f32, P]
+    L.gt_rope.argtypes = [ctypes.c_int] + [P] * 5 + [i64, i32, i32, ctypes.POINTER(GtRopeSpec), i32, P]
+    L.gt_layernorm_fwd.argtypes = [ctypes.c_int] + [P] * 6 + [i64, i32, f32, P]
+    L.gt_layernorm_bwd.argtypes = [ctypes.c_int] + [P] * 8 + [i64, i32, P]
+    for name in LAYER_SYMBOLS:
+        getattr(L, name).restype = ctypes.c_int
     for name in ("gt_attn_fwd", "gt_attn_fwd_bf16", "gt_attn_fwd_ex", "gt_attn_fwd_noalloc", "gt_gatv2_fwd",
                  "gt_attn_bwd",
                  "gt_segment_reduce", "gt_dot_aggr", "gt_csr_validate",
@@ -299,6 +314,141 @@ def gt_attn_bwd(rowptr, colidx, rowptr_t, colidx_t, Q, K, V, out, dout, lse, dQ,
                                       _ptr(dout), _ptr(lse), _ptr(dQ), _ptr(dK), _ptr(dV), N,
                                       colidx.numel(), H, D, float(scale),
                                       _stream(Q.device, stream)))
+
+
+def _feature_dtype(x):
+    if not isinstance(x, torch.Tensor):
+        raise TypeError("features must be torch tensors")
+    if x.dtype == torch.float32:
+        return GT_DTYPE_F32, (torch.float32,)
+    return GT_DTYPE_BF16, (torch.bfloat16, torch.int16, torch.uint16)
+
+
+def _check_features(device, dtypes, shape, **tensors):
+    """Contiguous device tensors of one shape, each of one of `dtypes`."""
+    for name, t in tensors.items():
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(name + " must be a torch.Tensor")
+        if not t.is_cuda or t.device != device:
+            raise ValueError("%s must be a device tensor on %s" % (name, device))
+        if not t.is_contiguous():
+            raise ValueError(name + " must be contiguous")
+        if t.dtype not in dtypes:
+            raise TypeError("%s: dtype %s not in %s" % (name, t.dtype, dtypes))
+        if tuple(t.shape) != tuple(shape):
+            raise ValueError("%s must have shape %s" % (name, list(shape)))
+
+
+def _check_csr(device, N, rowptr, colidx, names=("rowptr", "colidx")):
+    _check_features(device, (torch.int64,), (N + 1,), **{names[0]: rowptr})
+    if not isinstance(colidx, torch.Tensor) or colidx.dim() != 1:
+        raise ValueError(names[1] + " must be a one-dimensional tensor")
+    _check_features(device, (torch.int32,), colidx.shape, **{names[1]: colidx})
+
+
+def _diff_shape(Q):
+    if Q.dim() != 3 or Q.shape[1] % 2 != 0:
+        raise ValueError("Q must be [N, 2H, D]")
+    return Q.shape[0], Q.shape[1] // 2, Q.shape[2]
+
+
+def gt_diff_attn_fwd(rowptr, colidx, Q, K, V, lam, out, scale, tuning=None, stream=None, lse=None) -> None:
+    """Differential attention: out[i, h] = sum_e (softmax_e(s_0) - lam[h] softmax_e(s_1)) V[j_e, h] with
+    s_m = scale <Q[i, 2h + m], K[j_e, 2h + m]>.  Q, K: [N, 2H, D]; V, out: [N, H, 2D] (dtype from Q); lam: float32
+    [H]; lse: optional float32 [N, 2H], receives ln(sum_e exp(s)) of both maps.  See include/gt_layer.h."""
+    dtype, allowed = _feature_dtype(Q)
+    N, H, D = _diff_shape(Q)
+    _check_features(Q.device, allowed, Q.shape, Q=Q, K=K)
+    _check_features(Q.device, allowed, (N, H, 2 * D), V=V, out=out)
+    _check_features(Q.device, (torch.float32,), (H,), lam=lam)
+    _check_csr(Q.device, N, rowptr, colidx)
+    if lse is not None:
+        _check_features(Q.device, (torch.float32,), (N, 2 * H), lse=lse)
+    if isinstance(tuning, dict):
+        tuning = GtTuning(**tuning)
+    tp = ctypes.byref(tuning) if tuning is not None else None
+    _check(load_library().gt_diff_attn_fwd(dtype, _ptr(rowptr), _ptr(colidx), _ptr(Q), _ptr(K), _ptr(V), _ptr(lam),
+                                           _ptr(out), _ptr(lse), N, colidx.numel(), H, D, float(scale), tp,
+                                           _stream(Q.device, stream)))
+
+
+def gt_diff_attn_bwd(rowptr, colidx, rowptr_t, colidx_t, Q, K, V, lam, dout, lse, dQ, dK, dV, dlam, scale,
+                     stream=None) -> None:
+    """Gradients of sum(out * dout) of gt_diff_attn_fwd, from its lse; rowptr_t/colidx_t is the transposed structure
+    (sources as rows); dlam: float32 [H] or None.  See include/gt_layer.h."""
+    dtype, allowed = _feature_dtype(Q)
+    N, H, D = _diff_shape(Q)
+    _check_features(Q.device, allowed, Q.shape, Q=Q, K=K, dQ=dQ, dK=dK)
+    _check_features(Q.device, allowed, (N, H, 2 * D), V=V, dout=dout, dV=dV)
+    _check_features(Q.device, (torch.float32,), (H,), lam=lam)
+    if dlam is not None:
+        _check_features(Q.device, (torch.float32,), (H,), dlam=dlam)
+    _check_features(Q.device, (torch.float32,), (N, 2 * H), lse=lse)
+    _check_csr(Q.device, N, rowptr, colidx)
+    _check_csr(Q.device, N, rowptr_t, colidx_t, ("rowptr_t", "colidx_t"))
+    if colidx_t.numel() != colidx.numel():
+        raise ValueError("the transposed structure must have as many entries as the CSR")
+    _check(load_library().gt_diff_attn_bwd(dtype, _ptr(rowptr), _ptr(colidx), _ptr(rowptr_t), _ptr(colidx_t), _ptr(Q),
+                                           _ptr(K), _ptr(V), _ptr(lam), _ptr(dout), _ptr(lse), _ptr(dQ), _ptr(dK),
+                                           _ptr(dV), _ptr(dlam), N, colidx.numel(), H, D, float(scale),
+                                           _stream(Q.device, stream)))
+
+
+GT_ROPE_LAYOUTS = {"pairs": 0, "halves": 1, "sections": 2}
+
+
+def gt_rope(pos, Q, out_q, dims, K=None, out_k=None, theta=10000.0, layout="pairs", inverse=False,
+            stream=None) -> None:
+    """Rotary positions with several axes: turns the pairs of every head's elements by the angles that their node's
+    pos (float32 [N, axes]) gives; dims: elements that each axis turns; inverse: the other way, which is the gradient.
+    Q, out_q (and K, out_k): [N, H, D]; an output may be its own input.  See include/gt_layer.h."""
+    dtype, allowed = _feature_dtype(Q)
+    if Q.dim() != 3:
+        raise ValueError("Q must be [N, H, D]")
+    if (K is None) != (out_k is None):
+        raise ValueError("K and out_k must both be given, or neither")
+    N, H, D = Q.shape
+    _check_features(Q.device, allowed, Q.shape, Q=Q, out_q=out_q)
+    if K is not None:
+        _check_features(Q.device, allowed, Q.shape, K=K, out_k=out_k)
+    dims = [int(d) for d in dims]
+    if not 1 <= len(dims) <= 4:
+        raise ValueError("dims must have 1 to 4 axes")
+    _check_features(Q.device, (torch.float32,), (N, len(dims)), pos=pos)
+    spec = GtRopeSpec(len(dims), (ctypes.c_int32 * 4)(*dims), GT_ROPE_LAYOUTS[layout], float(theta))
+    _check(load_library().gt_rope(dtype, _ptr(pos), _ptr(Q), _ptr(K), _ptr(out_q), _ptr(out_k), N, H, D,
+                                  ctypes.byref(spec), 1 if inverse else 0, _stream(Q.device, stream)))
+
+
+def _norm_shape(X):
+    if not isinstance(X, torch.Tensor) or X.dim() != 2:
+        raise ValueError("X must be an [N, F] tensor")
+    return X.shape
+
+
+def gt_layernorm_fwd(X, gamma, beta, out, eps=1e-5, mean=None, rstd=None, stream=None) -> None:
+    """Layer norm of the rows of X [N, F] (dtype from X); gamma, beta: float32 [F] or None; mean, rstd: optional
+    float32 [N] of statistics for the backward; out may be X.  See include/gt_layer.h."""
+    N, F = _norm_shape(X)
+    dtype, allowed = _feature_dtype(X)
+    _check_features(X.device, allowed, X.shape, X=X, out=out)
+    _check_features(X.device, (torch.float32,), (F,), **{k: t for k, t in (("gamma", gamma), ("beta", beta)) if t is not None})
+    _check_features(X.device, (torch.float32,), (N,), **{k: t for k, t in (("mean", mean), ("rstd", rstd)) if t is not None})
+    _check(load_library().gt_layernorm_fwd(dtype, _ptr(X), _ptr(gamma), _ptr(beta), _ptr(out), _ptr(mean), _ptr(rstd),
+                                           N, F, float(eps), _stream(X.device, stream)))
+
+
+def gt_layernorm_bwd(X, dout, gamma, mean, rstd, dX, dgamma=None, dbeta=None, stream=None) -> None:
+    """Gradients of gt_layernorm_fwd from its mean and rstd; dgamma, dbeta: float32 [F] or None; dX may be X or dout.
+    See include/gt_layer.h."""
+    N, F = _norm_shape(X)
+    dtype, allowed = _feature_dtype(X)
+    _check_features(X.device, allowed, X.shape, X=X, dout=dout, dX=dX)
+    params = (("gamma", gamma), ("dgamma", dgamma), ("dbeta", dbeta))
+    _check_features(X.device, (torch.float32,), (F,), **{k: t for k, t in params if t is not None})
+    _check_features(X.device, (torch.float32,), (N,), mean=mean, rstd=rstd)
+    _check(load_library().gt_layernorm_bwd(dtype, _ptr(X), _ptr(dout), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(dX),
+                                           _ptr(dgamma), _ptr(dbeta), N, F, _stream(X.device, stream)))
 
 
 def attention(rowptr, colidx, Q, K, V, scale=None, tuning=None, out=None, stream=None,

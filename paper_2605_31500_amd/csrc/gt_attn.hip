@@ -31,6 +31,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <array>
 #include <atomic>
 #include <climits>
@@ -46,7 +47,7 @@
 #include <thread>
 #include <vector>
 
-#include "gt_attn.h"
+#include "gt_layer.h"
 
 // Workspace of the allocation-free entry point (gt_attn_fwd_noalloc): one
 // array per device, held from the library's load until the process ends.
@@ -134,6 +135,16 @@ template <> __device__ __forceinline__ uint4 narrow<bf16_tag>(const float* f) {
     return make_uint4(bf16_rne(f[0]) | (bf16_rne(f[1]) << 16), bf16_rne(f[2]) | (bf16_rne(f[3]) << 16),
                       bf16_rne(f[4]) | (bf16_rne(f[5]) << 16), bf16_rne(f[6]) | (bf16_rne(f[7]) << 16));
 }
+
+// Single elements, for rows that are no whole number of 16-byte vectors.
+template <typename T> struct Raw;
+template <> struct Raw<float> { typedef float type; };
+template <> struct Raw<bf16_tag> { typedef uint16_t type; };
+
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+__device__ __forceinline__ void from_f32(float x, float& y) { y = x; }
+__device__ __forceinline__ void from_f32(float x, uint16_t& y) { y = (uint16_t)bf16_rne(x); }
 
 // ---------------------------------------------------------- cross-lane sums
 
@@ -1791,6 +1802,21 @@ gt_status run_reduce(gt_dtype dtype, int op, const ReduceArgs& a0, const gt_tuni
     return fn(a, tu, stream);
 }
 
+#include "gt_diff.hpp"
+#include "gt_rope.hpp"
+#include "gt_norm.hpp"
+
+// No C++ exception leaves an entry point (host allocations of the messages and
+// of the workspace's bookkeeping may fail).
+template <typename F>
+gt_status guarded(F&& call) {
+    try {
+        return call();
+    } catch (...) {
+        return GT_ERROR_OUT_OF_MEMORY;
+    }
+}
+
 #include "gt_study.hpp"
 
 gt_status run_dot_aggr(const int64_t* rowptr, const int32_t* colidx, const float* X, float* out, int64_t N,
@@ -1869,6 +1895,89 @@ gt_status gt_segment_reduce(gt_dtype dtype, gt_reduce_op op, const int64_t* rowp
                             const void* X, void* out, int32_t* arg, int64_t N, int64_t E, int32_t F,
                             const gt_tuning* tuning, hipStream_t stream) {
     return run_reduce(dtype, (int)op, ReduceArgs{rowptr, colidx, X, out, arg, N, E, F, 0u}, tuning, stream);
+}
+
+gt_status gt_diff_attn_fwd(gt_dtype dtype, const int64_t* rowptr, const int32_t* colidx, const void* Q, const void* K,
+                           const void* V, const float* lambda, void* out, float* lse, int64_t N, int64_t E, int32_t H,
+                           int32_t D, float scale, const gt_tuning* tuning, hipStream_t stream) {
+    DiffArgs a{};
+    a.rowptr = rowptr;
+    a.colidx = colidx;
+    a.Q = Q;
+    a.K = K;
+    a.V = V;
+    a.lambda = lambda;
+    a.out = out;
+    a.lse_out = lse;
+    a.N = N;
+    a.E = E;
+    a.H = H;
+    a.D = D;
+    a.scale = scale;
+    return guarded([&] { return run_diff(dtype, a, false, tuning, stream); });
+}
+
+gt_status gt_diff_attn_bwd(gt_dtype dtype, const int64_t* rowptr, const int32_t* colidx, const int64_t* rowptr_t,
+                           const int32_t* colidx_t, const void* Q, const void* K, const void* V, const float* lambda,
+                           const void* dout, const float* lse, void* dQ, void* dK, void* dV, float* dlambda, int64_t N,
+                           int64_t E, int32_t H, int32_t D, float scale, hipStream_t stream) {
+    DiffArgs a{};
+    a.rowptr = rowptr;
+    a.colidx = colidx;
+    a.rowptr_t = rowptr_t;
+    a.colidx_t = colidx_t;
+    a.Q = Q;
+    a.K = K;
+    a.V = V;
+    a.lambda = lambda;
+    a.dout = dout;
+    a.lse = lse;
+    a.dQ = dQ;
+    a.dK = dK;
+    a.dV = dV;
+    a.dlambda = dlambda;
+    a.N = N;
+    a.E = E;
+    a.H = H;
+    a.D = D;
+    a.scale = scale;
+    return guarded([&] { return run_diff(dtype, a, true, nullptr, stream); });
+}
+
+gt_status gt_rope(gt_dtype dtype, const float* pos, const void* Q, const void* K, void* outQ, void* outK, int64_t N,
+                  int32_t H, int32_t D, const gt_rope_spec* spec, int32_t inverse, hipStream_t stream) {
+    return guarded([&] { return run_rope(dtype, pos, Q, K, outQ, outK, N, H, D, spec, inverse, stream); });
+}
+
+gt_status gt_layernorm_fwd(gt_dtype dtype, const void* X, const float* gamma, const float* beta, void* out, float* mean,
+                           float* rstd, int64_t N, int32_t F, float eps, hipStream_t stream) {
+    NormArgs a{};
+    a.X = X;
+    a.gamma = gamma;
+    a.beta = beta;
+    a.out = out;
+    a.mean = mean;
+    a.rstd = rstd;
+    a.N = N;
+    a.F = F;
+    a.eps = eps;
+    return guarded([&] { return run_norm(dtype, a, false, stream); });
+}
+
+gt_status gt_layernorm_bwd(gt_dtype dtype, const void* X, const void* dout, const float* gamma, const float* mean,
+                           const float* rstd, void* dX, float* dgamma, float* dbeta, int64_t N, int32_t F, hipStream_t stream) {
+    NormArgs a{};
+    a.X = X;
+    a.dout = dout;
+    a.gamma = gamma;
+    a.mean_in = mean;
+    a.rstd_in = rstd;
+    a.out = dX;
+    a.dgamma = dgamma;
+    a.dbeta = dbeta;
+    a.N = N;
+    a.F = F;
+    return guarded([&] { return run_norm(dtype, a, true, stream); });
 }
 
 gt_status gt_dot_aggr(const int64_t* rowptr, const int32_t* colidx, const float* X, float* out, int64_t N,
