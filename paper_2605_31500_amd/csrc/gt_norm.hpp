@@ -4,6 +4,11 @@
 //     out  = (x - mean) rstd gamma + beta
 //     dX   = rstd (g - mean(g) - x^ mean(g x^)),  g = dout gamma, x^ = (x - mean) rstd
 //     dgamma = sum over rows of dout x^, dbeta = sum over rows of dout
+// A row is read once and kept in registers between its sums and its output, so a
+// call moves what it has to and is bound by HBM (1 M rows of 256 bf16 elements:
+// forward 198 us, 5.5 TB/s; 169 K rows of 512 fp32: backward 183 us, 5.7 TB/s, of
+// which the parameters' gradients' second kernel is 3), small calls by their
+// launches (2000 rows of 128 fp32: 3.9 us).
 
 struct NormArgs {
     const void* X;
@@ -24,130 +29,438 @@ struct NormArgs {
 
 constexpr int32_t kNormMaxF = 16384;
 
-// One wavefront per row.
-template <typename T>
-__global__ void __launch_bounds__(kBlock) gt_norm_fwd_kernel(NormArgs a) {
-    typedef typename Raw<T>::type R;
-    const int lane = threadIdx.x & (kWave - 1);
-    for (int64_t row = (int64_t)blockIdx.x * kWavesPerBlock + threadIdx.x / kWave; row < a.N; row += (int64_t)gridDim.x * kWavesPerBlock) {
-    const R* x = static_cast<const R*>(a.X) + row * a.F;
-    R* y = static_cast<R*>(a.out) + row * a.F;
-    float s = 0.0f;
-    for (int f = lane; f < a.F; f += kWave) s += to_f32(x[f]);
-    const float mean = head_sum<64>(s) / (float)a.F;
-    float v = 0.0f;
-    for (int f = lane; f < a.F; f += kWave) {
-        const float d = to_f32(x[f]) - mean;
-        v = fmaf(d, d, v);
-    }
-    const float rstd = 1.0f / sqrtf(head_sum<64>(v) / (float)a.F + a.eps);
-    for (int f = lane; f < a.F; f += kWave) {
-        const float h = (to_f32(x[f]) - mean) * rstd;
-        from_f32(fmaf(h, a.gamma ? a.gamma[f] : 1.0f, a.beta ? a.beta[f] : 0.0f), y[f]);
-    }
-    if (lane == 0) {
-        if (a.mean) a.mean[row] = mean;
-        if (a.rstd) a.rstd[row] = rstd;
-    }
-    }
-}
+// A row is read once, into registers, by G lanes with K accesses of 16 bytes (W
+// elements) each.  Rows that are no whole number of 16 bytes (ODD) start inside
+// one: `phase` elements of the row before it are read along and masked, and the
+// first and last access of a row store single elements.  A group's rows are all
+// of one phase, so that its accesses hold the same columns in every row.
+typedef uint32_t NormVec __attribute__((ext_vector_type(4)));
 
-template <typename T>
-__global__ void __launch_bounds__(kBlock) gt_norm_bwd_kernel(NormArgs a) {
-    typedef typename Raw<T>::type R;
-    const int lane = threadIdx.x & (kWave - 1);
-    for (int64_t row = (int64_t)blockIdx.x * kWavesPerBlock + threadIdx.x / kWave; row < a.N; row += (int64_t)gridDim.x * kWavesPerBlock) {
-    const R* x = static_cast<const R*>(a.X) + row * a.F;
-    const R* dy = static_cast<const R*>(a.dout) + row * a.F;
-    R* dx = static_cast<R*>(a.out) + row * a.F;
-    const float mean = a.mean_in[row], rstd = a.rstd_in[row];
-    float s1 = 0.0f, s2 = 0.0f;
-    for (int f = lane; f < a.F; f += kWave) {
-        const float g = to_f32(dy[f]) * (a.gamma ? a.gamma[f] : 1.0f);
-        s1 += g;
-        s2 = fmaf(g, (to_f32(x[f]) - mean) * rstd, s2);
-    }
-    s1 = head_sum<64>(s1) / (float)a.F;
-    s2 = head_sum<64>(s2) / (float)a.F;
-    for (int f = lane; f < a.F; f += kWave) {
-        const float g = to_f32(dy[f]) * (a.gamma ? a.gamma[f] : 1.0f), h = (to_f32(x[f]) - mean) * rstd;
-        from_f32(rstd * (g - s1 - h * s2), dx[f]);
-    }
-    }
-}
+template <typename T, int G_, int K_, bool ODD>
+struct NormRow {
+    static constexpr int G = G_, K = K_, W = 16 / Elt<T>::kBytes;
+    static constexpr int kThreads = G > kBlock ? G : kBlock;
+    static constexpr int kGroups = kThreads / G;  // of a workgroup
+    static constexpr int kAhead = G > kWave || K > 2 ? 1 : 4 / K;  // rows that a group requests together
+    static constexpr int kAheadBwd = K * W > 8 ? 1 : ODD ? (kAhead + 1) / 2 : kAhead;
+    // parameters stay in registers (read again for every row, us: backward of 60 K rows of
+    // 1000 bf16 113 against 77)
+    static constexpr bool kKeep = K * W <= (ODD ? 16 : 32);
+    NormVec v[K];
 
-// Parameters' gradients: a workgroup sums a stretch of rows for 64 columns,
-// the second kernel the stretches.
-constexpr int kNormStretches = 256;
+    // Column of the first element of access k.
+    __device__ __forceinline__ static int column(int lig, int k, int phase) { return (lig + k * G) * W - (ODD ? phase : 0); }
+    __device__ __forceinline__ static bool holds(int col, int e, int32_t F) {
+        return ODD ? (uint32_t)(col + e) < (uint32_t)F : col < F;
+    }
 
-template <typename T>
-__global__ void __launch_bounds__(kBlock) gt_norm_param_kernel(NormArgs a, float* part) {
-    typedef typename Raw<T>::type R;
-    __shared__ float sums[2][kWavesPerBlock][kWave];
-    const int lane = threadIdx.x & (kWave - 1), wv = threadIdx.x / kWave;
-    const int f = blockIdx.x * kWave + lane;
-    const int64_t lo = a.N * blockIdx.y / gridDim.y, hi = a.N * (blockIdx.y + 1) / gridDim.y;
-    float sg = 0.0f, sb = 0.0f;
-    if (f < a.F)
-        for (int64_t i = lo + wv; i < hi; i += kWavesPerBlock) {
-            const float dy = to_f32(static_cast<const R*>(a.dout)[i * a.F + f]);
-            const float x = to_f32(static_cast<const R*>(a.X)[i * a.F + f]);
-            sg = fmaf(dy, (x - a.mean_in[i]) * a.rstd_in[i], sg);
-            sb += dy;
+    // (elements of other rows are read as 0)
+    __device__ __forceinline__ void load(const void* base, int64_t N, int64_t row, int32_t F, int lig, int phase) {
+        typedef typename Raw<T>::type R;
+        const R* p = static_cast<const R*>(base) + row * F;
+        const int64_t left = (N - row) * F;  // elements up to the tensor's end
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int c = column(lig, k, phase);
+            v[k] = NormVec{0, 0, 0, 0};
+            if (c >= F || (ODD && c + W <= 0)) continue;
+            if (ODD && c + W > left) {  // (nothing past the end)
+#pragma unroll
+                for (int e = 0; e < W; ++e) {
+                    if (!holds(c, e, F)) continue;
+                    if constexpr (W == 4)
+                        v[k][e] = __float_as_uint(p[c + e]);
+                    else
+                        v[k][e / 2] |= (uint32_t)p[c + e] << (e % 2 * 16);
+                }
+            } else {
+                // past the caches, unless two rows share lines (plain loads throughout / past
+                // the caches, us: backward of 169 K rows of 512 fp32 194 / 183, of 60 K rows of
+                // 203 bf16 26.0 / 31.0; a choice at run time costs the former 9)
+                const NormVec* at = reinterpret_cast<const NormVec*>(p + c);
+                v[k] = ODD ? *at : __builtin_nontemporal_load(at);
+                if constexpr (ODD) {
+#pragma unroll
+                    for (int d = 0; d < 4; ++d)
+                        if constexpr (W == 4)
+                            v[k][d] = holds(c, d, F) ? v[k][d] : 0u;
+                        else
+                            v[k][d] &= (holds(c, 2 * d, F) ? 0x0000FFFFu : 0u) | (holds(c, 2 * d + 1, F) ? 0xFFFF0000u : 0u);
+                }
+            }
         }
-    sums[0][wv][lane] = sg;
-    sums[1][wv][lane] = sb;
+    }
+
+    __device__ __forceinline__ void elements(int k, float (&x)[W]) const {
+        widen<T>(make_uint4(v[k][0], v[k][1], v[k][2], v[k][3]), x);
+    }
+
+    __device__ __forceinline__ static void store(void* base, int64_t row, int32_t F, int lig, int phase, int k, const float (&x)[W]) {
+        typedef typename Raw<T>::type R;
+        R* p = static_cast<R*>(base) + row * F;
+        const int c = column(lig, k, phase);
+        if (c >= F || (ODD && c + W <= 0)) return;
+        NormVec o;
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+            if constexpr (W == 4)
+                o[d] = __float_as_uint(x[d]);
+            else
+                o[d] = pack_bf16(x[2 * d], x[2 * d + 1]);
+        if (ODD && (c < 0 || c + W > F)) {
+#pragma unroll
+            for (int e = 0; e < W; ++e)
+                if (holds(c, e, F)) {
+                    if constexpr (W == 4)
+                        p[c + e] = x[e];
+                    else
+                        p[c + e] = (R)(o[e / 2] >> (e % 2 * 16));
+                }
+        } else if constexpr (ODD) {
+            // (rows share lines: left to the L2 to put together)
+            *reinterpret_cast<NormVec*>(p + c) = o;
+        } else {
+            __builtin_nontemporal_store(o, reinterpret_cast<NormVec*>(p + c));
+        }
+    }
+
+    // Parameters at access k (`other` where there are none).
+    __device__ __forceinline__ static void params(const float* base, int32_t F, int lig, int phase, int k, float other, float (&x)[W]) {
+        const int c = column(lig, k, phase);
+#pragma unroll
+        for (int e = 0; e < W; ++e) x[e] = base && holds(c, e, F) ? base[c + e] : other;
+    }
+};
+
+// The rows of a group: `first` and every `step` after it, and with each of them
+// the next ones `apart`.  A workgroup's rows follow one another, unless those of
+// a group would be of different phases then (ODD: the grid is a multiple of 8).
+// (Rows that a group requests together apart by the grid, fp32 and bf16 alike:
+// 1 M rows of 256 bf16 elements 214 us against 198.)
+template <typename Row, bool ODD, int AHEAD>
+struct NormRows {
+    static constexpr bool kTogether = !ODD || Row::kGroups % Row::W == 0;
+    int64_t first, step, apart;
+    int phase;
+    __device__ __forceinline__ NormRows(int32_t F, int g) {
+        first = (int64_t)blockIdx.x * Row::kGroups * (kTogether ? AHEAD : 1) + g;
+        step = (int64_t)gridDim.x * Row::kGroups * AHEAD;
+        apart = kTogether ? Row::kGroups : (int64_t)gridDim.x * Row::kGroups;
+        phase = ODD ? (int)((first % Row::W) * (F % Row::W) % Row::W) : 0;
+    }
+};
+
+// Sums of M values over the G lanes of a row's group, in every lane.
+template <int G, int M>
+__device__ __forceinline__ void group_sum(float (&x)[M], float* lds, int& turn) {
+    if constexpr (G <= kWave) {
+#pragma unroll
+        for (int m = 0; m < M; ++m) x[m] = head_sum<G>(x[m]);
+    } else {
+        // (two buffers in turn: a sum's readers are done before the next but one is written)
+        constexpr int kWaves = G / kWave;
+        float* buf = lds + turn * kWaves * M;
+        turn ^= 1;
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+            x[m] = head_sum<kWave>(x[m]);
+            if (threadIdx.x % kWave == 0) buf[m * kWaves + threadIdx.x / kWave] = x[m];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+            x[m] = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) x[m] += buf[m * kWaves + w];
+        }
+    }
+}
+
+template <typename T, int G, int K, bool ODD>
+__global__ void __launch_bounds__((NormRow<T, G, K, ODD>::kThreads)) gt_norm_fwd_kernel(NormArgs a) {
+    using Row = NormRow<T, G, K, ODD>;
+    constexpr int W = Row::W;
+    constexpr int kAhead = Row::kAhead;
+    __shared__ float lds[G > kWave ? 2 * G / kWave : 1];
+    int turn = 0;
+    const int lig = threadIdx.x % G, g = threadIdx.x / G;
+    const float inv_f = 1.0f / (float)a.F;
+    const NormRows<Row, ODD, kAhead> rows(a.F, g);
+    constexpr bool kKeep = Row::kKeep;
+    float gm[kKeep ? K : 1][W], bt[kKeep ? K : 1][W];
+    if constexpr (kKeep)
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            Row::params(a.gamma, a.F, lig, rows.phase, k, 1.0f, gm[k]);
+            Row::params(a.beta, a.F, lig, rows.phase, k, 0.0f, bt[k]);
+        }
+    // (uniform where the group is more than a wavefront)
+    for (int64_t r0 = rows.first; r0 < a.N; r0 += rows.step) {
+        Row x[kAhead];
+#pragma unroll
+        for (int b = 0; b < kAhead; ++b) {
+            const int64_t row = r0 + b * rows.apart;
+            x[b].load(a.X, a.N, row < a.N ? row : r0, a.F, lig, rows.phase);
+        }
+#pragma unroll
+        for (int b = 0; b < kAhead; ++b) {
+            const int64_t row = r0 + b * rows.apart;
+            float s[1] = {0.0f};
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                float e[W];
+                x[b].elements(k, e);
+#pragma unroll
+                for (int i = 0; i < W; ++i) s[0] += e[i];
+            }
+            group_sum<G, 1>(s, lds, turn);
+            const float mean = s[0] * inv_f;
+            float q[1] = {0.0f};
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                float e[W];
+                x[b].elements(k, e);
+#pragma unroll
+                for (int i = 0; i < W; ++i) {
+                    const float d = Row::holds(Row::column(lig, k, rows.phase), i, a.F) ? e[i] - mean : 0.0f;
+                    q[0] = fmaf(d, d, q[0]);
+                }
+            }
+            group_sum<G, 1>(q, lds, turn);
+            const float rstd = 1.0f / sqrtf(fmaf(q[0], inv_f, a.eps));
+            if (row >= a.N) continue;
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                float e[W], o[W];
+                x[b].elements(k, e);
+                if constexpr (!kKeep) {
+                    Row::params(a.gamma, a.F, lig, rows.phase, k, 1.0f, gm[0]);
+                    Row::params(a.beta, a.F, lig, rows.phase, k, 0.0f, bt[0]);
+                }
+#pragma unroll
+                for (int i = 0; i < W; ++i) o[i] = fmaf((e[i] - mean) * rstd, gm[kKeep ? k : 0][i], bt[kKeep ? k : 0][i]);
+                Row::store(a.out, row, a.F, lig, rows.phase, k, o);
+            }
+            if (lig == 0) {
+                if (a.mean) a.mean[row] = mean;
+                if (a.rstd) a.rstd[row] = rstd;
+            }
+        }
+    }
+}
+
+// Backward.  A group sums its rows' shares of the parameters' gradients in
+// registers; at the end they are added over the groups of the workgroup, which
+// leaves one partial row each of dgamma and dbeta in `part` [workgroup][2][F].
+template <typename T, int G, int K, bool ODD>
+__global__ void __launch_bounds__((NormRow<T, G, K, ODD>::kThreads)) gt_norm_bwd_kernel(NormArgs a, float* part) {
+    using Row = NormRow<T, G, K, ODD>;
+    constexpr int W = Row::W;
+    constexpr int kAhead = Row::kAheadBwd;
+    constexpr int kLdsSum = G > kWave ? 4 * G / kWave : 0, kLdsParam = Row::kGroups > 1 ? Row::kThreads * K * W : 0;
+    __shared__ float lds[kLdsSum > kLdsParam ? kLdsSum : kLdsParam > 0 ? kLdsParam : 1];
+    int turn = 0;
+    const int lig = threadIdx.x % G, g = threadIdx.x / G;
+    const float inv_f = 1.0f / (float)a.F;
+    float sg[K][W], sb[K][W];
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int i = 0; i < W; ++i) sg[k][i] = sb[k][i] = 0.0f;
+    const NormRows<Row, ODD, kAhead> rows(a.F, g);
+    constexpr bool kKeep = Row::kKeep;
+    float gm[kKeep ? K : 1][W];
+    if constexpr (kKeep)
+#pragma unroll
+        for (int k = 0; k < K; ++k) Row::params(a.gamma, a.F, lig, rows.phase, k, 1.0f, gm[k]);
+    // (uniform where the group is more than a wavefront)
+    for (int64_t r0 = rows.first; r0 < a.N; r0 += rows.step) {
+        Row x[kAhead], y[kAhead];
+        float mean[kAhead], rstd[kAhead];
+#pragma unroll
+        for (int b = 0; b < kAhead; ++b) {
+            const int64_t row = r0 + b * rows.apart, at = row < a.N ? row : r0;
+            x[b].load(a.X, a.N, at, a.F, lig, rows.phase);
+            y[b].load(a.dout, a.N, at, a.F, lig, rows.phase);
+            mean[b] = a.mean_in[at];
+            rstd[b] = a.rstd_in[at];
+        }
+#pragma unroll
+        for (int b = 0; b < kAhead; ++b) {
+            const int64_t row = r0 + b * rows.apart;
+            if (row >= a.N) break;
+            // x^ = x rstd - mean rstd (as near as the rounded mean itself is)
+            const float shift = -mean[b] * rstd[b];
+            float s[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                float ex[W], ey[W];
+                x[b].elements(k, ex);
+                y[b].elements(k, ey);
+                if constexpr (!kKeep) Row::params(a.gamma, a.F, lig, rows.phase, k, 1.0f, gm[0]);
+#pragma unroll
+                for (int i = 0; i < W; ++i) {  // (dout is 0 outside the row)
+                    const float h = fmaf(ex[i], rstd[b], shift), gr = ey[i] * gm[kKeep ? k : 0][i];
+                    s[0] += gr;
+                    s[1] = fmaf(gr, h, s[1]);
+                    sg[k][i] = fmaf(ey[i], h, sg[k][i]);
+                    sb[k][i] += ey[i];
+                }
+            }
+            group_sum<G, 2>(s, lds, turn);
+            const float m1 = -rstd[b] * (s[0] * inv_f), m2 = -rstd[b] * (s[1] * inv_f);
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                float ex[W], ey[W], o[W];
+                x[b].elements(k, ex);
+                y[b].elements(k, ey);
+                if constexpr (!kKeep) Row::params(a.gamma, a.F, lig, rows.phase, k, 1.0f, gm[0]);
+#pragma unroll
+                for (int i = 0; i < W; ++i) {
+                    const float h = fmaf(ex[i], rstd[b], shift), gr = ey[i] * gm[kKeep ? k : 0][i];
+                    o[i] = fmaf(gr, rstd[b], fmaf(h, m2, m1));
+                }
+                Row::store(a.out, row, a.F, lig, rows.phase, k, o);
+            }
+        }
+    }
+    if (!part) return;
+    float* dst = part + (int64_t)blockIdx.x * 2 * a.F;
+    if constexpr (Row::kGroups == 1) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int c = Row::column(lig, k, rows.phase);
+#pragma unroll
+            for (int i = 0; i < W; ++i)
+                if (Row::holds(c, i, a.F)) {
+                    dst[c + i] = sg[k][i];
+                    dst[a.F + c + i] = sb[k][i];
+                }
+        }
+    } else {
+        constexpr int kCols = G * K * W;
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const int c = Row::column(lig, k, rows.phase);
+#pragma unroll
+                for (int i = 0; i < W; ++i)
+                    if (Row::holds(c, i, a.F)) lds[g * kCols + c + i] = which ? sb[k][i] : sg[k][i];
+            }
+            __syncthreads();
+            for (int c = threadIdx.x; c < a.F; c += Row::kThreads) {
+                float x = lds[c];
+                for (int o = 1; o < Row::kGroups; ++o) x += lds[o * kCols + c];
+                dst[which * a.F + c] = x;
+            }
+        }
+    }
+}
+
+// The workgroups' partial rows, added in 64 bits in a fixed order: 16 columns
+// (a 64-byte piece of every row) and 64 stretches of the rows to a workgroup.
+constexpr int kNormCols = 16, kNormStretches = 64;
+
+__global__ void __launch_bounds__(kNormCols * kNormStretches)
+gt_norm_param_kernel(const float* part, int blocks, int32_t F, float* dgamma, float* dbeta) {
+    __shared__ double sums[kNormStretches][kNormCols];
+    const int c = threadIdx.x % kNormCols, r = threadIdx.x / kNormCols, col = blockIdx.x * kNormCols + c;
+    double s = 0.0;
+    if (col < 2 * F)
+#pragma unroll 8
+        for (int b = r; b < blocks; b += kNormStretches) s += part[(int64_t)b * 2 * F + col];
+    sums[r][c] = s;
     __syncthreads();
-    if (wv < 2 && f < a.F)
-        part[((int64_t)blockIdx.y * 2 + wv) * a.F + f] =
-            (sums[wv][0][lane] + sums[wv][1][lane]) + (sums[wv][2][lane] + sums[wv][3][lane]);
-}
-
-__global__ void __launch_bounds__(kBlock) gt_norm_param_sum_kernel(const float* part, int stretches, int32_t F, float* dgamma,
-                                                                   float* dbeta) {
-    const int f = blockIdx.x * kBlock + threadIdx.x;
-    if (f >= F) return;
-    double sg = 0.0, sb = 0.0;
-    for (int s = 0; s < stretches; ++s) {
-        sg += part[(int64_t)s * 2 * F + f];
-        sb += part[((int64_t)s * 2 + 1) * F + f];
+    if (r < kNormCols) {
+#pragma unroll
+        for (int i = kNormCols; i < kNormStretches; i += kNormCols) s += sums[r + i][c];
+        sums[r][c] = s;
     }
-    if (dgamma) dgamma[f] = (float)sg;
-    if (dbeta) dbeta[f] = (float)sb;
+    __syncthreads();
+    if (r != 0 || col >= 2 * F) return;
+#pragma unroll
+    for (int i = 1; i < kNormCols; ++i) s += sums[i][c];
+    float* dst = col < F ? dgamma : dbeta;
+    if (dst) dst[col < F ? col : col - F] = (float)s;
 }
 
-template <typename T>
-gt_status launch_norm_fwd(const NormArgs& a, hipStream_t stream) {
-    const int64_t blocks = std::min<int64_t>((a.N + kWavesPerBlock - 1) / kWavesPerBlock, 1 << 20);
-    hipLaunchKernelGGL(gt_norm_fwd_kernel<T>, dim3((unsigned)blocks), dim3(kBlock), 0, stream, a);
-    const hipError_t he = hipGetLastError();
-    return he == hipSuccess ? GT_SUCCESS : hip_fail(he, "layer norm launch");
+// Workgroups: all that the device holds at once (each keeps its parameters and
+// sums for many rows), or one for the rows that its groups request together.
+template <typename T, int G, int K, bool ODD, bool BACKWARD>
+int norm_blocks(int64_t rows_per_block, int64_t N, int dev) {
+    static std::atomic<int> cache[64];
+    int most = dev >= 0 && dev < 64 ? cache[dev].load() : 0;
+    if (most == 0) {
+        int nb = 0;
+        const void* kernel = BACKWARD ? reinterpret_cast<const void*>(gt_norm_bwd_kernel<T, G, K, ODD>)
+                                      : reinterpret_cast<const void*>(gt_norm_fwd_kernel<T, G, K, ODD>);
+        if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&nb, kernel, NormRow<T, G, K, ODD>::kThreads, 0) != hipSuccess || nb <= 0) nb = 1;
+        most = nb * device_cus(dev);
+        if (dev >= 0 && dev < 64) cache[dev] = most;
+    }
+    int64_t need = (N + rows_per_block - 1) / rows_per_block;
+    if (need > most) need = most;
+    return (int)(ODD ? (need + 7) / 8 * 8 : need);
 }
 
-template <typename T>
-gt_status launch_norm_bwd(const NormArgs& a, int dev, hipStream_t stream) {
+template <typename T, int G, int K, bool ODD>
+gt_status launch_norm(const NormArgs& a, bool backward, int dev, hipStream_t stream) {
+    using Row = NormRow<T, G, K, ODD>;
     hipError_t he = hipSuccess;
-    if (a.dgamma || a.dbeta) {
-        // (before dX, which may be one of its inputs)
-        const int stretches = (int)(a.N < kNormStretches ? a.N : kNormStretches);
-        CallWorkspace cw;
-        if (const gt_status st = acquire_workspace(dev, (size_t)(stretches > 0 ? stretches : 1) * 2 * a.F * sizeof(float), stream, cw);
-            st != GT_SUCCESS)
-            return st;
-        float* part = reinterpret_cast<float*>(cw.ptr);
-        if (stretches > 0) {
-            hipLaunchKernelGGL(gt_norm_param_kernel<T>, dim3((a.F + kWave - 1) / kWave, stretches), dim3(kBlock), 0, stream, a, part);
-            if ((he = hipGetLastError()) != hipSuccess) return hip_fail(he, "layer norm parameter launch");
-        }
-        hipLaunchKernelGGL(gt_norm_param_sum_kernel, dim3((a.F + kBlock - 1) / kBlock), dim3(kBlock), 0, stream, part, stretches, a.F,
+    if (!backward) {
+        const int blocks = norm_blocks<T, G, K, ODD, false>(Row::kGroups * Row::kAhead, a.N, dev);
+        hipLaunchKernelGGL((gt_norm_fwd_kernel<T, G, K, ODD>), dim3(blocks), dim3(Row::kThreads), 0, stream, a);
+        he = hipGetLastError();
+        return he == hipSuccess ? GT_SUCCESS : hip_fail(he, "layer norm launch");
+    }
+    const int blocks = norm_blocks<T, G, K, ODD, true>(Row::kGroups * Row::kAheadBwd, a.N, dev);
+    CallWorkspace cw;
+    if (a.dgamma || a.dbeta)
+        if (const gt_status st = acquire_workspace(dev, (size_t)blocks * 2 * a.F * sizeof(float), stream, cw); st != GT_SUCCESS) return st;
+    float* part = reinterpret_cast<float*>(cw.ptr);
+    hipLaunchKernelGGL((gt_norm_bwd_kernel<T, G, K, ODD>), dim3(blocks), dim3(Row::kThreads), 0, stream, a, part);
+    if ((he = hipGetLastError()) != hipSuccess) return hip_fail(he, "layer norm backward launch");
+    if (part) {
+        hipLaunchKernelGGL(gt_norm_param_kernel, dim3((2 * a.F + kNormCols - 1) / kNormCols), dim3(kNormCols * kNormStretches), 0, stream, part, blocks, a.F,
                            a.dgamma, a.dbeta);
         if ((he = hipGetLastError()) != hipSuccess) return hip_fail(he, "layer norm parameter launch");
     }
-    if (a.N == 0) return GT_SUCCESS;
-    const int64_t blocks = std::min<int64_t>((a.N + kWavesPerBlock - 1) / kWavesPerBlock, 1 << 20);
-    hipLaunchKernelGGL(gt_norm_bwd_kernel<T>, dim3((unsigned)blocks), dim3(kBlock), 0, stream, a);
-    he = hipGetLastError();
-    return he == hipSuccess ? GT_SUCCESS : hip_fail(he, "layer norm backward launch");
+    return GT_SUCCESS;
+}
+
+// The lanes of a row by its accesses (ODD: with those of the largest phase).  A
+// wavefront takes rows of up to four accesses per lane, since a row of more
+// wavefronts waits for their sums; masks cost ODD rows more registers, which get
+// more lanes instead.
+template <typename T, bool ODD>
+gt_status pick_norm(const NormArgs& a, bool backward, int dev, hipStream_t stream) {
+    constexpr int W = 16 / Elt<T>::kBytes;
+    const int32_t c = (a.F + (ODD ? W - 1 : 0) + W - 1) / W;
+    if (c <= 8) return launch_norm<T, 8, 1, ODD>(a, backward, dev, stream);
+    if (c <= 16) return launch_norm<T, 16, 1, ODD>(a, backward, dev, stream);
+    if (c <= 32) return launch_norm<T, 32, 1, ODD>(a, backward, dev, stream);
+    if (c <= 64) return launch_norm<T, 64, 1, ODD>(a, backward, dev, stream);
+    if (c <= 128) return launch_norm<T, 64, 2, ODD>(a, backward, dev, stream);
+    if (c <= 256) return launch_norm<T, ODD ? 256 : 64, ODD ? 1 : 4, ODD>(a, backward, dev, stream);
+    if (c <= 512) return launch_norm<T, 256, 2, ODD>(a, backward, dev, stream);
+    if (c <= 1024) return launch_norm<T, ODD ? 512 : 256, ODD ? 2 : 4, ODD>(a, backward, dev, stream);
+    if (c <= 2048) return launch_norm<T, ODD ? 1024 : 512, ODD ? 2 : 4, ODD>(a, backward, dev, stream);
+    if constexpr (W == 4 || ODD) return launch_norm<T, 1024, W == 8 ? 3 : ODD ? 5 : 4, ODD>(a, backward, dev, stream);
+    return GT_ERROR_NOT_SUPPORTED;  // (kNormMaxF)
+}
+
+template <typename T>
+gt_status dispatch_norm(const NormArgs& a, bool backward, int dev, hipStream_t stream) {
+    if (a.N == 0) {  // (0.0f is all bits 0)
+        for (float* p : {a.dgamma, a.dbeta})
+            if (p)
+                if (const hipError_t he = clear_counters(reinterpret_cast<int32_t*>(p), a.F, stream); he != hipSuccess)
+                    return hip_fail(he, "layer norm parameter launch");
+        return GT_SUCCESS;
+    }
+    return a.F % (16 / Elt<T>::kBytes) == 0 ? pick_norm<T, false>(a, backward, dev, stream) : pick_norm<T, true>(a, backward, dev, stream);
 }
 
 gt_status run_norm(gt_dtype dtype, const NormArgs& a, bool backward, hipStream_t stream) {
@@ -199,6 +512,5 @@ gt_status run_norm(gt_dtype dtype, const NormArgs& a, bool backward, hipStream_t
     if (a.N == 0 && !a.dgamma && !a.dbeta) return GT_SUCCESS;
     int dev = 0;
     if (const gt_status ds = call_device(stream, &dev); ds != GT_SUCCESS) return ds;
-    if (!backward) return dtype == GT_DTYPE_F32 ? launch_norm_fwd<float>(a, stream) : launch_norm_fwd<bf16_tag>(a, stream);
-    return dtype == GT_DTYPE_F32 ? launch_norm_bwd<float>(a, dev, stream) : launch_norm_bwd<bf16_tag>(a, dev, stream);
+    return dtype == GT_DTYPE_F32 ? dispatch_norm<float>(a, backward, dev, stream) : dispatch_norm<bf16_tag>(a, backward, dev, stream);
 }
