@@ -2,7 +2,12 @@
 // anonymous namespace): pairs (x, y) of a head's elements are turned by
 // t = pos[node][axis] theta^-e, in every head alike:
 //     (x, y) <- (x cos t - y sin t, x sin t + y cos t)
-// The angle is formed and reduced to a part of a turn in 64 bits.
+// The angle is formed and reduced to a part of a turn in 64 bits.  Each element is
+// read and written once: bound by HBM (1 M nodes, Q and K of 8x64 bf16 by three
+// axes in halves of 8 and 12 elements: 815 us, 5.3 TB/s; in whole 16-byte accesses
+// the same), small calls by the chain of position, table and rows (16 K nodes of
+// 4x32 fp32: 8.0 us).  Non-temporal accesses: 1089 us, since an access' lines are
+// shared by the halves' other one.
 
 constexpr int kRopeAxes = 4;
 constexpr int kRopeMaxD = 512;
@@ -19,6 +24,8 @@ struct RopeParams {
     int32_t dims[kRopeAxes];
     int32_t layout;
     int32_t turned;     // sum of dims
+    int32_t nodes;   // of a workgroup at a time
+    int32_t copies;  // the elements past the turned ones are copied
     double log2_theta;
     float sign;  // -1: turn back
 };
@@ -56,41 +63,221 @@ __device__ __forceinline__ RopePair rope_pair(const RopeParams& r, int p) {
     return q;
 }
 
-// One thread per node and pair.
-template <typename T>
+// A workgroup takes `nodes` nodes at a time.  It forms their angles' sines and
+// cosines once, into LDS, and then runs over their rows of Q and K with 16-byte
+// accesses (W elements; 8, 4 or 2 bytes where pairs do not come in whole ones), so
+// that every head's pairs share one evaluation and the rows move as in a copy.
+//
+// The elements of a head are turned by units: W neighbours (PAIRS), or W and
+// the W elements that they are paired with.  Elements past the turned ones are
+// units of their own, which are copied unless the call is in place.  What a
+// unit is, the workgroup writes into LDS once.
+typedef uint32_t RopeVec4 __attribute__((ext_vector_type(4)));
+typedef uint32_t RopeVec2 __attribute__((ext_vector_type(2)));
+template <int BYTES> struct RopeAccess;
+template <> struct RopeAccess<16> { typedef RopeVec4 type; };
+template <> struct RopeAccess<8> { typedef RopeVec2 type; };
+template <> struct RopeAccess<4> { typedef uint32_t type; };
+template <> struct RopeAccess<2> { typedef uint16_t type; };
+
+template <typename T, int W> struct RopeUnit {
+    typedef typename RopeAccess<W * Elt<T>::kBytes>::type Vec;
+    __device__ __forceinline__ static void widen_to(const Vec& v, float (&x)[W]) {
+        typename Raw<T>::type r[W];
+        __builtin_memcpy(r, &v, sizeof v);
+#pragma unroll
+        for (int e = 0; e < W; ++e) x[e] = to_f32(r[e]);
+    }
+    __device__ __forceinline__ static Vec narrow_from(const float (&x)[W]) {
+        Vec v;
+        if constexpr (std::is_same<T, float>::value || W == 1) {
+            typename Raw<T>::type r[W];
+#pragma unroll
+            for (int e = 0; e < W; ++e) from_f32(x[e], r[e]);
+            __builtin_memcpy(&v, r, sizeof v);
+        } else {
+            uint32_t r[W / 2];
+#pragma unroll
+            for (int e = 0; e < W; e += 2) r[e / 2] = pack_bf16(x[e], x[e + 1]);
+            __builtin_memcpy(&v, r, sizeof v);
+        }
+        return v;
+    }
+};
+
+// Sine and cosine of `turns` whole turns: less the nearest quarter turn in 64
+// bits, so that what is rounded to fp32 is at most an eighth of a turn, and then
+// the Taylor polynomials in the rest's radians r, |r| <= pi / 4 (their next terms
+// are below 2^-28: r^11 / 11! and r^12 / 12!).
+__device__ __forceinline__ float2 rope_cos_sin(double turns) {
+    const double quarters = 4.0 * turns, q = rint(quarters);
+    const float r = (float)((quarters - q) * 1.5707963267948966), r2 = r * r;
+    const int k = (int)(q - 4.0 * floor(0.25 * q)) & 3;  // (NaN: any)
+    float s = fmaf(r2, 2.7557319e-6f, -1.9841270e-4f);
+    s = fmaf(r2, s, 8.3333333e-3f);
+    s = fmaf(r2, s, -1.6666667e-1f);
+    s = fmaf(r * r2, s, r);
+    float c = fmaf(r2, -2.7557319e-7f, 2.4801587e-5f);
+    c = fmaf(r2, c, -1.3888889e-3f);
+    c = fmaf(r2, c, 4.1666667e-2f);
+    c = fmaf(r2, c, -0.5f);
+    c = fmaf(r2, c, 1.0f);
+    const float cs = k & 1 ? s : c, sn = k & 1 ? c : s;
+    return make_float2(k == 1 || k == 2 ? -cs : cs, k >= 2 ? -sn : sn);
+}
+
+constexpr int kRopeTable = 2048;    // pairs' sines and cosines at a time
+constexpr int kRopeHeld = 1 << 16;  // units of a tensor at a time
+constexpr int kRopeUnits = 8;       // that a thread requests together
+
+// i / d by a multiplication, for i < 2^16 and d <= 2^16 (i e < 2^32, with e <= d
+// what the factor's rounding adds).
+struct Quotient {
+    uint32_t factor;
+    __device__ __forceinline__ explicit Quotient(int d) : factor(d == 1 ? 0u : 0xFFFFFFFFu / (uint32_t)d + 1u) {}
+    __device__ __forceinline__ int operator()(int i) const { return factor ? (int)__umulhi((uint32_t)i, factor) : i; }
+};
+
+template <typename T, int W, bool PAIRS>
 __global__ void __launch_bounds__(kBlock) gt_rope_kernel(RopeParams r) {
     typedef typename Raw<T>::type R;
+    using Unit = RopeUnit<T, W>;
+    typedef typename Unit::Vec Vec;
+    __shared__ float2 table[kRopeTable];
+    __shared__ double freq[kRopeMaxD / 2];
+    __shared__ int32_t axis[kRopeMaxD / 2];
+    __shared__ int32_t first[kRopeMaxD / W], second[kRopeMaxD / W], pair[kRopeMaxD / W];  // of each unit; pair -1: copied
     const int half = r.turned / 2;
-    const int64_t node = blockIdx.x;
     for (int p = threadIdx.x; p < half; p += kBlock) {
         const RopePair q = rope_pair(r, p);
-        double turns = (double)r.pos[node * r.axes + q.axis] * q.freq;
-        turns -= rint(turns);
-        float sn, cs;
-        sincospif(2.0f * (float)turns, &sn, &cs);
-        sn *= r.sign;
-        for (int t = 0; t < 2; ++t) {
-            const R* src = static_cast<const R*>(t ? r.K : r.Q);
-            R* dst = static_cast<R*>(t ? r.outK : r.outQ);
-            if (!src) continue;
-            for (int h = 0; h < r.H; ++h) {
-                const int64_t at = (node * r.H + h) * r.D;
-                const float x = to_f32(src[at + q.lo]), y = to_f32(src[at + q.hi]);
-                from_f32(x * cs - y * sn, dst[at + q.lo]);
-                from_f32(x * sn + y * cs, dst[at + q.hi]);
+        freq[p] = q.freq;
+        axis[p] = q.axis;
+        if (PAIRS ? q.lo % W == 0 : p % W == 0) {
+            const int u = PAIRS ? q.lo / W : p / W;
+            first[u] = q.lo;
+            second[u] = q.hi;
+            pair[u] = p;
+        }
+    }
+    const int turned_units = PAIRS ? r.turned / W : half / W, units = r.copies ? turned_units + (r.D - r.turned) / W : turned_units;
+    for (int u = turned_units + threadIdx.x; u < units; u += kBlock) {
+        first[u] = second[u] = r.turned + (u - turned_units) * W;
+        pair[u] = -1;
+    }
+    const int tensors = r.K ? 2 : 1, per_node = r.H * units;
+    const Quotient by_half(half), by_units(units), by_heads(r.H);
+    for (int64_t n0 = (int64_t)blockIdx.x * r.nodes; n0 < r.N; n0 += (int64_t)gridDim.x * r.nodes) {
+        const int nodes = (int)(r.N - n0 < r.nodes ? r.N - n0 : r.nodes);
+        __syncthreads();  // (the units and frequencies are there, the table's readers done)
+        for (int i = threadIdx.x; i < nodes * half; i += kBlock) {
+            const int n = by_half(i), p = i - n * half;
+            float2 cs = rope_cos_sin((double)r.pos[(n0 + n) * r.axes + axis[p]] * freq[p]);
+            cs.y *= r.sign;
+            table[i] = cs;
+        }
+        __syncthreads();
+        // (the units of Q, then those of K: requested together)
+        const int each = nodes * per_node, total = tensors * each;
+        const int64_t row0 = n0 * r.H * r.D;
+        for (int i0 = threadIdx.x; i0 < total; i0 += kRopeUnits * kBlock) {
+            Vec a[kRopeUnits], b[PAIRS ? 1 : kRopeUnits];
+            int at[kRopeUnits], bt[kRopeUnits], cs[kRopeUnits];
+#pragma unroll
+            for (int j = 0; j < kRopeUnits; ++j) {
+                int i = i0 + j * kBlock < total ? i0 + j * kBlock : i0;  // (past the last: read and left)
+                const bool key = i >= each;
+                if (key) i -= each;
+                const R* src = static_cast<const R*>(key ? r.K : r.Q) + row0;
+                const int head = by_units(i), u = i - head * units;
+                at[j] = head * r.D + first[u];
+                bt[j] = head * r.D + second[u];
+                cs[j] = pair[u] < 0 ? -1 : by_heads(head) * half + pair[u];
+                a[j] = *reinterpret_cast<const Vec*>(src + at[j]);
+                if constexpr (!PAIRS) b[j] = *reinterpret_cast<const Vec*>(src + bt[j]);
+            }
+#pragma unroll
+            for (int j = 0; j < kRopeUnits; ++j) {
+                if (i0 + j * kBlock >= total) break;
+                R* dst = static_cast<R*>(i0 + j * kBlock >= each ? r.outK : r.outQ) + row0;
+                if (cs[j] < 0) {
+                    *reinterpret_cast<Vec*>(dst + at[j]) = a[j];
+                    continue;
+                }
+                const float2* c = table + cs[j];
+                float x[W], ox[W];
+                Unit::widen_to(a[j], x);
+                if constexpr (PAIRS) {
+#pragma unroll
+                    for (int e = 0; e < W; e += 2) {
+                        ox[e] = x[e] * c[e / 2].x - x[e + 1] * c[e / 2].y;
+                        ox[e + 1] = x[e] * c[e / 2].y + x[e + 1] * c[e / 2].x;
+                    }
+                } else {
+                    float y[W], oy[W];
+                    Unit::widen_to(b[j], y);
+#pragma unroll
+                    for (int e = 0; e < W; ++e) {
+                        ox[e] = x[e] * c[e].x - y[e] * c[e].y;
+                        oy[e] = x[e] * c[e].y + y[e] * c[e].x;
+                    }
+                    *reinterpret_cast<Vec*>(dst + bt[j]) = Unit::narrow_from(oy);
+                }
+                *reinterpret_cast<Vec*>(dst + at[j]) = Unit::narrow_from(ox);
             }
         }
     }
-    const int rest = r.D - r.turned;
-    for (int t = 0; t < 2; ++t) {
-        const R* src = static_cast<const R*>(t ? r.K : r.Q);
-        R* dst = static_cast<R*>(t ? r.outK : r.outQ);
-        if (!src || src == dst) continue;
-        for (int i = threadIdx.x; i < rest * r.H; i += kBlock) {
-            const int64_t at = (node * r.H + i / rest) * r.D + r.turned + i % rest;
-            dst[at] = src[at];
+}
+
+// Elements of an access: the most, up to 16 bytes, that divide every stretch of
+// elements which lie together with their partners, and the rest of the head.
+int rope_access(const RopeParams& r, int elt_bytes) {
+    int w = 16 / elt_bytes;
+    auto fit = [&w](int n) {
+        while (n % w != 0) w /= 2;
+    };
+    fit(r.D);
+    fit(r.D - r.turned);
+    int off = 0;
+    for (int a = 0; a < r.axes; ++a) {
+        if (r.layout == GT_ROPE_PAIRS) {
+            fit(off);
+        } else if (r.layout == GT_ROPE_HALVES) {
+            fit(off);
+            fit(r.dims[a] / 2);
         }
+        off += r.dims[a];
     }
+    if (r.layout == GT_ROPE_SECTIONS) fit(off / 2);
+    return w;
+}
+
+template <typename T, int W, bool PAIRS>
+gt_status launch_rope(RopeParams r, int dev, hipStream_t stream) {
+    // nodes of a workgroup: as many as the table holds, fewer where the call has not enough for the device
+    const int64_t most = kRopeTable / (r.turned / 2), even = (r.N + 4 * device_cus(dev) - 1) / (4 * device_cus(dev));
+    const int64_t held = kRopeHeld / ((int64_t)r.H * r.D / W) > 0 ? kRopeHeld / ((int64_t)r.H * r.D / W) : 1;
+    r.nodes = (int32_t)std::min(std::min(even, most), held);
+    const int64_t blocks = std::min<int64_t>((r.N + r.nodes - 1) / r.nodes, 8 * device_cus(dev));
+    hipLaunchKernelGGL((gt_rope_kernel<T, W, PAIRS>), dim3((unsigned)blocks), dim3(kBlock), 0, stream, r);
+    const hipError_t he = hipGetLastError();
+    return he == hipSuccess ? GT_SUCCESS : hip_fail(he, "rotary launch");
+}
+
+template <typename T>
+gt_status pick_rope(const RopeParams& r, int dev, hipStream_t stream) {
+    constexpr int kMost = 16 / Elt<T>::kBytes;
+    const int w = rope_access(r, Elt<T>::kBytes);
+    if (r.layout == GT_ROPE_PAIRS) {  // (w is even: so are the sections)
+        if constexpr (kMost == 8)
+            if (w == 8) return launch_rope<T, 8, true>(r, dev, stream);
+        if (w == 4) return launch_rope<T, 4, true>(r, dev, stream);
+        return launch_rope<T, 2, true>(r, dev, stream);
+    }
+    if constexpr (kMost == 8)
+        if (w == 8) return launch_rope<T, 8, false>(r, dev, stream);
+    if (w == 4) return launch_rope<T, 4, false>(r, dev, stream);
+    if (w == 2) return launch_rope<T, 2, false>(r, dev, stream);
+    return launch_rope<T, 1, false>(r, dev, stream);
 }
 
 gt_status run_rope(gt_dtype dtype, const float* pos, const void* Q, const void* K, void* outQ, void* outK, int64_t N,
@@ -141,21 +328,6 @@ gt_status run_rope(gt_dtype dtype, const float* pos, const void* Q, const void* 
     r.layout = (int32_t)spec->layout;
     r.log2_theta = std::log2(spec->theta);
     r.sign = inverse ? -1.0f : 1.0f;
-    for (int64_t n0 = 0; n0 < N; n0 += 1 << 23) {  // (a launch holds fewer than 2^32 threads)
-        RopeParams s = r;
-        const int64_t at = n0 * H * D * (dtype == GT_DTYPE_F32 ? 4 : 2);
-        s.pos += n0 * r.axes;
-        s.Q = static_cast<const char*>(Q) + at;
-        s.K = K ? static_cast<const char*>(K) + at : nullptr;
-        s.outQ = static_cast<char*>(outQ) + at;
-        s.outK = outK ? static_cast<char*>(outK) + at : nullptr;
-        s.N = N - n0 < (1 << 23) ? N - n0 : 1 << 23;
-        if (dtype == GT_DTYPE_F32)
-            hipLaunchKernelGGL(gt_rope_kernel<float>, dim3((unsigned)s.N), dim3(kBlock), 0, stream, s);
-        else
-            hipLaunchKernelGGL(gt_rope_kernel<bf16_tag>, dim3((unsigned)s.N), dim3(kBlock), 0, stream, s);
-        const hipError_t he = hipGetLastError();
-        if (he != hipSuccess) return hip_fail(he, "rotary launch");
-    }
-    return GT_SUCCESS;
+    r.copies = r.turned < D && (outQ != Q || outK != K);
+    return dtype == GT_DTYPE_F32 ? pick_rope<float>(r, dev, stream) : pick_rope<bf16_tag>(r, dev, stream);
 }
