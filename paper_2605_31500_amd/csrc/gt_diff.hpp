@@ -40,6 +40,7 @@ struct DiffParams {
     int32_t maps;    // 2H
     int32_t slice0;  // slice of blockIdx.y == 0
     float* part;     // [slice of this launch][slot][kSlotFloats]
+    int32_t* zero;   // a counter that the kernel without a partition clears, or nullptr
 };
 
 // What the lanes share while a wavefront works on one slice: base pointers at
@@ -526,35 +527,124 @@ __global__ void __launch_bounds__(kBlock) gt_diff_merge_kernel(DiffParams p) {
     }
 }
 
-// dlambda[h] = - sum over rows of Delta_1: partial sums per workgroup, then
-// their sum, in 64 bits and a fixed order.
-constexpr int kLambdaBlocks = 256;
+// Small graphs, without a partition: a workgroup takes as many rows as it has
+// lane groups, in id order.  A group reads a row of up to kDirectAlone entries by
+// itself; longer ones are then read one after another by all groups of the
+// workgroup, a share each, and merged in LDS in a fixed order.  One launch takes
+// the place of three (clear and partition, rows, merge).
+constexpr uint32_t kDirectAlone = 48;
 
-__global__ void __launch_bounds__(kBlock) gt_diff_lambda_kernel(const float2* stat, int64_t N, int32_t H, double* part) {
-    __shared__ double sums[kBlock];
-    const int h = threadIdx.x % H, r = threadIdx.x / H, per = kBlock / H;
-    double s = 0.0;
-    for (int64_t i = (int64_t)blockIdx.x * per + r; i < N; i += (int64_t)gridDim.x * per) s -= stat[(i * H + h) * 2 + 1].y;
-    sums[threadIdx.x] = s;
-    __syncthreads();
-    for (int off = kBlock / 2; off >= H; off >>= 1) {
-        if ((int)threadIdx.x < off) sums[threadIdx.x] += sums[threadIdx.x + off];
-        __syncthreads();
+template <typename Op, typename T, int PS, int D>
+__global__ void __launch_bounds__(kBlock) gt_diff_direct_kernel(DiffParams p) {
+    constexpr int G = Op::kG, P = kWave / G, U = Op::kU;
+    constexpr uint32_t kGroups = kWavesPerBlock * P;
+    __shared__ __attribute__((aligned(16))) float parts[kWavesPerBlock * Op::kSlotFloats];
+    __shared__ uint64_t long_rows[kWavesPerBlock];
+    const int lane = threadIdx.x & (kWave - 1), wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int lig = lane % G;
+    const uint32_t group = wv * P + lane / G;
+    Op op = diff_op<Op, T, PS, D>(p);
+    op.part = parts;
+    auto entries = [&](typename Op::State& st, uint32_t begin, uint32_t end) {
+        int32_t j[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) j[u] = p.w.colidx[begin + u < end ? begin + u : end - 1];
+        for (uint32_t t = begin; t < end; t += U) {
+            typename Op::State::Batch bt;
+            st.issue(op, j, lig, bt);
+            int32_t next[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) next[u] = p.w.colidx[t + U + u < end ? t + U + u : end - 1];
+            st.consume(op, bt, j, end - t < (uint32_t)U ? (int)(end - t) : U);
+#pragma unroll
+            for (int u = 0; u < U; ++u) j[u] = next[u];
+        }
+    };
+
+    if (p.zero && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.zero = 0;
+    const int64_t row0 = (int64_t)blockIdx.x * kGroups, row = row0 + group;
+    uint32_t begin = 0, end = 0;
+    if (row < p.w.N) {
+        begin = (uint32_t)p.w.rowptr[row];
+        end = (uint32_t)p.w.rowptr[row + 1];
     }
-    if ((int)threadIdx.x < H) part[blockIdx.x * H + threadIdx.x] = sums[threadIdx.x];
+    const bool alone = end - begin <= kDirectAlone;
+    const uint64_t longs = __ballot(!alone && lig == 0);
+    if (lane == 0) long_rows[wv] = longs;
+    if (row < p.w.N && alone) {
+        typename Op::State st;
+        st.reset();
+        st.begin(op, (int32_t)row, lig);
+        if (end > begin) entries(st, begin, end);
+        st.store_out(op, (int32_t)row, lig);
+    }
+    __syncthreads();
+    for (int w = 0; w < kWavesPerBlock; ++w) {
+        for (uint64_t left = long_rows[w]; left; left &= left - 1) {
+            const int64_t r = row0 + w * P + __builtin_ctzll(left) / G;
+            const uint32_t rb = (uint32_t)p.w.rowptr[r], deg = (uint32_t)p.w.rowptr[r + 1] - rb;
+            const uint32_t b = rb + (uint32_t)((uint64_t)deg * group / kGroups), e = rb + (uint32_t)((uint64_t)deg * (group + 1) / kGroups);
+            typename Op::State st;
+            st.reset();
+            st.begin(op, (int32_t)r, lig);
+            if (e > b) entries(st, b, e);
+#pragma unroll
+            for (int off = G; off < kWave; off <<= 1) st.merge_xor(off);
+            if (lane < G) st.store_partial(op, wv, lig);
+            __syncthreads();
+            if (wv == 0) {
+                st.reset();
+#pragma unroll
+                for (int k = 0; k < kWavesPerBlock; ++k) {
+                    typename Op::State::Partial pt;
+                    st.load_partial(op, k, lig, pt);
+                    st.add(pt, true);
+                }
+                if (lane < G) st.store_out(op, (int32_t)r, lig);
+            }
+            __syncthreads();
+        }
+    }
 }
 
-__global__ void __launch_bounds__(kBlock) gt_diff_lambda_sum_kernel(const double* part, int blocks, int32_t H, float* dlambda) {
+// dlambda[h] = - sum over rows of Delta_1, in 64 bits: partial sums per
+// workgroup, which the last workgroup to finish adds, in a fixed order.
+constexpr int kLambdaBlocks = 256;
+
+__global__ void __launch_bounds__(kBlock) gt_diff_lambda_kernel(const float2* stat, int64_t N, int32_t H, double* part, int32_t* done,
+                                                                float* dlambda) {
     __shared__ double sums[kBlock];
-    const int h = threadIdx.x % H, per = kBlock / H;
-    double s = 0.0;
-    for (int b = threadIdx.x / H; b < blocks; b += per) s += part[b * H + h];
-    sums[threadIdx.x] = s;
-    __syncthreads();
-    for (int off = kBlock / 2; off >= H; off >>= 1) {
-        if ((int)threadIdx.x < off) sums[threadIdx.x] += sums[threadIdx.x + off];
+    __shared__ int last;
+    const int h = threadIdx.x % H, r = threadIdx.x / H, per = kBlock / H;
+    auto reduce = [&](double s) {  // over the threads of a head, to the first
+        sums[threadIdx.x] = s;
         __syncthreads();
+        for (int off = kBlock / 2; off >= H; off >>= 1) {
+            if ((int)threadIdx.x < off) sums[threadIdx.x] += sums[threadIdx.x + off];
+            __syncthreads();
+        }
+    };
+    double s = 0.0;
+    const int64_t step = (int64_t)gridDim.x * per;
+#pragma unroll 4
+    for (int64_t i = (int64_t)blockIdx.x * per + r; i < N; i += step) s -= stat[(i * H + h) * 2 + 1].y;
+    reduce(s);
+    if (gridDim.x == 1) {
+        if ((int)threadIdx.x < H) dlambda[threadIdx.x] = (float)sums[threadIdx.x];
+        return;
     }
+    if ((int)threadIdx.x < H) {
+        __hip_atomic_store(part + blockIdx.x * H + threadIdx.x, sums[threadIdx.x], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __threadfence();
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) last = __hip_atomic_fetch_add(done, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    s = 0.0;
+    for (int b = r; b < (int)gridDim.x; b += per) s += __hip_atomic_load(part + b * H + h, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    reduce(s);
     if ((int)threadIdx.x < H) dlambda[threadIdx.x] = (float)sums[threadIdx.x];
 }
 
@@ -613,6 +703,25 @@ gt_status launch_diff_rows(DiffParams dp, const RowRule& rule, const SlotPlan& s
     return GT_SUCCESS;
 }
 
+// Whether a call takes its rows without a partition: small graphs, as long as
+// their hubs' chains stay shorter than the launches saved (with a partition /
+// without, us per call: forward of 2 K nodes of degree 9 fp32 1x32 20 / 11, power
+// law of 4 K nodes (27 K entries) 25.5 / 19.3, of 8 K nodes (64 K) 26 / 43, 1.5 K
+// R-MAT nodes (36 K) 25 / 22; bf16 4x64, power law of 1.5 K nodes (8 K) 26 / 13, of
+// 4 K nodes 34 / 39; backward: 49 / 38, 54 / 84, 50 / 55, 55 / 32, 65 / 72).
+bool diff_direct(int64_t N, int64_t E, int64_t row_bytes, const gt_tuning* tu) {
+    return !tu && N <= 4096 && E <= 32768 && E * row_bytes <= (int64_t(16) << 20);
+}
+
+template <typename Op, typename T, int PS, int D>
+gt_status launch_diff_direct(const DiffParams& dp, hipStream_t stream) {
+    constexpr int kGroups = kWavesPerBlock * (kWave / Op::kG);
+    hipLaunchKernelGGL((gt_diff_direct_kernel<Op, T, PS, D>), dim3((unsigned)((dp.w.N + kGroups - 1) / kGroups), dp.maps / (2 * PS)), dim3(kBlock),
+                       0, stream, dp);
+    const hipError_t he = hipGetLastError();
+    return he == hipSuccess ? GT_SUCCESS : hip_fail(he, "differential attention launch");
+}
+
 // Workspace: two counter sets | statistics | light rows | long rows | partial
 // states | partial sums of dlambda.
 struct DiffPlan {
@@ -626,7 +735,7 @@ DiffPlan plan_diff(const DiffArgs& a, int gather_bytes, int slot_bytes, bool bac
     DiffPlan p;
     const int slices = a.H / PS;
     p.rule = row_rule(a.N, a.E, slices, gather_bytes, backward ? 2 * slot_bytes + 1024 : 3 * (2 * slot_bytes + 256) / 4, Op::Gm::kP, tu);
-    size_t off = align_up(2 * kRowsSetWords * sizeof(int32_t), 256);
+    size_t off = align_up((2 * kRowsSetWords + kRowsStride) * sizeof(int32_t), 256);  // (and a counter)
     auto place = [&off](size_t bytes) {
         const size_t at = off;
         off = align_up(off + bytes, 256);
@@ -660,26 +769,55 @@ void diff_work(RowWork& w, const DiffArgs& a, const DiffPlan& plan, char* ws) {
 }
 
 template <typename T, int PS, int D>
+void diff_features(DiffParams& dp, const DiffArgs& a) {
+    dp.lambda = a.lambda;
+    dp.lse = a.lse;
+    dp.c = a.scale * 1.4426950408889634f;
+    dp.scale = a.scale;
+    dp.row_shift = floor_log2((uint64_t)2 * a.H * a.D * Elt<T>::kBytes);
+    dp.maps = 2 * a.H;
+}
+
+template <typename T, int PS, int D>
 gt_status launch_diff_fwd(const DiffArgs& a, const gt_tuning* tu, hipStream_t stream) {
     using Op = DiffFwdOp<T, PS, D>;
     constexpr int kSlotBytes = Op::kSlotFloats * (int)sizeof(float);
-    const DiffPlan plan = plan_diff<Op, PS>(a, 2 * Op::kRow * Elt<T>::kBytes, kSlotBytes, false, tu);
     int dev = 0;
     if (const gt_status ds = call_device(stream, &dev); ds != GT_SUCCESS) return ds;
+    hipError_t he = hipSuccess;
+    DiffParams dp{};
+    diff_features<T, PS, D>(dp, a);
+    dp.A = static_cast<const char*>(a.Q);
+    dp.B = dp.A;
+    dp.X = static_cast<const char*>(a.K);
+    dp.Y = static_cast<const char*>(a.V);
+    dp.lse_out = a.lse_out;
+    dp.out1 = static_cast<char*>(a.out);
+    dp.out2 = dp.out1;
+    PhaseEvents ph;
+    if (diff_direct(a.N, a.E, (int64_t)2 * a.H * a.D * Elt<T>::kBytes, tu)) {
+        dp.w.rowptr = a.rowptr;
+        dp.w.colidx = a.colidx;
+        dp.w.N = a.N;
+        if ((he = ph.start(stream)) != hipSuccess) return hip_fail(he, "profiling events");
+        ph.mark(1, stream);
+        if (const gt_status st = launch_diff_direct<Op, T, PS, D>(dp, stream); st != GT_SUCCESS) return st;
+        ph.mark(2, stream);
+        ph.commit(stream);
+        return GT_SUCCESS;
+    }
+    const DiffPlan plan = plan_diff<Op, PS>(a, 2 * Op::kRow * Elt<T>::kBytes, kSlotBytes, false, tu);
     const RowGrid rg = row_grid(a.N, a.E, Op::Gm::kP, plan.slots.slices, false, diff_resident<Op, T, PS, D>(dev), tu);
     CallWorkspace cw;
     gt_status st = acquire_workspace(dev, plan.bytes, stream, cw);
     if (st != GT_SUCCESS) return st;
-    hipError_t he = hipSuccess;
-    DiffParams dp{};
     diff_work<Op>(dp.w, a, plan, cw.ptr);
+    dp.part = reinterpret_cast<float*>(cw.ptr + plan.o_part);
     // counter sets as in the attention forward: a cached block alternates between
     // its two, and the partition clears the one of the block's next call
     int32_t* cnt = reinterpret_cast<int32_t*>(cw.ptr);
     const bool alternate = cw.kind == CallWorkspace::CACHED;
     dp.w.counters = cnt + (alternate ? (cw.block.gen & 1u) * kRowsSetWords : 0);
-
-    PhaseEvents ph;
     if ((he = ph.start(stream)) != hipSuccess) return hip_fail(he, "profiling events");
     if (!(alternate && cw.block.primed) && (he = clear_counters(dp.w.counters, kRowsSetWords, stream)) != hipSuccess)
         return hip_fail(he, "counter clear");
@@ -694,19 +832,6 @@ gt_status launch_diff_fwd(const DiffArgs& a, const gt_tuning* tu, hipStream_t st
         cw.keep_primed = true;
     }
     ph.mark(1, stream);
-    dp.A = static_cast<const char*>(a.Q);
-    dp.B = dp.A;
-    dp.X = static_cast<const char*>(a.K);
-    dp.Y = static_cast<const char*>(a.V);
-    dp.lambda = a.lambda;
-    dp.lse_out = a.lse_out;
-    dp.out1 = static_cast<char*>(a.out);
-    dp.out2 = dp.out1;
-    dp.c = a.scale * 1.4426950408889634f;
-    dp.scale = a.scale;
-    dp.row_shift = floor_log2((uint64_t)2 * a.H * a.D * Elt<T>::kBytes);
-    dp.maps = 2 * a.H;
-    dp.part = reinterpret_cast<float*>(cw.ptr + plan.o_part);
     st = launch_diff_rows<Op, T, PS, D>(dp, plan.rule, plan.slots, rg, dev, &ph, stream);
     if (st != GT_SUCCESS) return st;
     ph.commit(stream);
@@ -729,6 +854,7 @@ template <typename T, int PS, int D>
 gt_status launch_diff_bwd(const DiffArgs& a, const gt_tuning*, hipStream_t stream) {
     using Op = DiffBwdOp<T, PS, D, 0>;
     constexpr int kSlotBytes = Op::kSlotFloats * (int)sizeof(float);  // (pass 1: the accumulators alone)
+    const bool direct = diff_direct(a.N, a.E, (int64_t)2 * a.H * a.D * Elt<T>::kBytes, nullptr);
     const DiffPlan plan = plan_diff<Op, PS>(a, 2 * Op::kRow * Elt<T>::kBytes, kSlotBytes, true, nullptr);
     int dev = 0;
     if (const gt_status ds = call_device(stream, &dev); ds != GT_SUCCESS) return ds;
@@ -736,18 +862,18 @@ gt_status launch_diff_bwd(const DiffArgs& a, const gt_tuning*, hipStream_t strea
     gt_status st = acquire_workspace(dev, plan.bytes, stream, cw);
     if (st != GT_SUCCESS) return st;
     int32_t* cnt = reinterpret_cast<int32_t*>(cw.ptr);
+    int32_t* done = cnt + 2 * kRowsSetWords;
     hipError_t he = hipSuccess;
-    if ((he = clear_counters(cnt, 2 * kRowsSetWords, stream)) != hipSuccess) return hip_fail(he, "counter clear");
+    const int64_t per = kBlock / a.H * 8;
+    const int blocks = (int)(a.N / per + 1 < kLambdaBlocks ? a.N / per + 1 : kLambdaBlocks);
+    if (!direct && (he = clear_counters(cnt, 2 * kRowsSetWords + kRowsStride, stream)) != hipSuccess)
+        return hip_fail(he, "counter clear");
     DiffParams dp{};
     diff_work<Op>(dp.w, a, plan, cw.ptr);
-    dp.lambda = a.lambda;
-    dp.lse = a.lse;
+    diff_features<T, PS, D>(dp, a);
     dp.stat = reinterpret_cast<float2*>(cw.ptr + plan.o_stat);
-    dp.c = a.scale * 1.4426950408889634f;
-    dp.scale = a.scale;
-    dp.row_shift = floor_log2((uint64_t)2 * a.H * a.D * Elt<T>::kBytes);
-    dp.maps = 2 * a.H;
     dp.part = reinterpret_cast<float*>(cw.ptr + plan.o_part);
+    dp.zero = done;
     for (int mode = 0; mode < 2; ++mode) {
         dp.w.rowptr = mode == 0 ? a.rowptr : a.rowptr_t;
         dp.w.colidx = mode == 0 ? a.colidx : a.colidx_t;
@@ -758,17 +884,17 @@ gt_status launch_diff_bwd(const DiffArgs& a, const gt_tuning*, hipStream_t strea
         dp.Y = static_cast<const char*>(mode == 0 ? a.V : a.dout);
         dp.out1 = static_cast<char*>(mode == 0 ? a.dQ : a.dK);
         dp.out2 = static_cast<char*>(a.dV);
-        st = mode == 0 ? launch_diff_bwd_pass<T, PS, D, 0>(dp, a, plan, dev, stream)
-                       : launch_diff_bwd_pass<T, PS, D, 1>(dp, a, plan, dev, stream);
+        if (direct)
+            st = mode == 0 ? launch_diff_direct<DiffBwdOp<T, PS, D, 0>, T, PS, D>(dp, stream)
+                           : launch_diff_direct<DiffBwdOp<T, PS, D, 1>, T, PS, D>(dp, stream);
+        else
+            st = mode == 0 ? launch_diff_bwd_pass<T, PS, D, 0>(dp, a, plan, dev, stream)
+                           : launch_diff_bwd_pass<T, PS, D, 1>(dp, a, plan, dev, stream);
         if (st != GT_SUCCESS) return st;
     }
     if (a.dlambda) {
-        double* part = reinterpret_cast<double*>(cw.ptr + plan.o_lambda);
-        const int64_t per = kBlock / a.H * 8;
-        const int blocks = (int)(a.N / per + 1 < kLambdaBlocks ? a.N / per + 1 : kLambdaBlocks);
-        hipLaunchKernelGGL(gt_diff_lambda_kernel, dim3(blocks), dim3(kBlock), 0, stream, dp.stat, a.N, a.H, part);
-        if ((he = hipGetLastError()) != hipSuccess) return hip_fail(he, "lambda gradient launch");
-        hipLaunchKernelGGL(gt_diff_lambda_sum_kernel, dim3(1), dim3(kBlock), 0, stream, part, blocks, a.H, a.dlambda);
+        hipLaunchKernelGGL(gt_diff_lambda_kernel, dim3(blocks), dim3(kBlock), 0, stream, dp.stat, a.N, a.H,
+                           reinterpret_cast<double*>(cw.ptr + plan.o_lambda), done, a.dlambda);
         if ((he = hipGetLastError()) != hipSuccess) return hip_fail(he, "lambda gradient launch");
     }
     return GT_SUCCESS;

@@ -27,6 +27,15 @@ def inputs(seed, N, H, D, dtype, graph=None, std=1.0):
     return rowptr, colidx, Q, K, V.reshape(N, H, 2 * D), lam, dO, np.float32(1 / math.sqrt(D))
 
 
+def larger_graph(seed, H, D, dtype):
+    """Enough rows and entries that the call partitions its rows: short rows, hubs, empty rows."""
+    row = 2 * H * D * (4 if dtype == "f32" else 2)
+    entries = min(32768, (16 << 20) // row) + 1000
+    N = max(600, entries // 12)
+    return synth.ragged_graph(seed, N, max_deg=24, empty_frac=0.1, hubs={7: 599, 100: 150, 299: 70}, self_loops=True, dup_frac=0.05,
+                              shuffle=True)
+
+
 def run_fwd(rowptr, colidx, Q, K, V, lam, scale, tuning=None, want_lse=True):
     import torch
     import paper_2605_31500_amd as gt
@@ -83,6 +92,14 @@ def test_forward(H, D, dtype, split):
 @pytest.mark.parametrize("H,D,dtype", CASES)
 def test_backward(H, D, dtype):
     check_bwd(inputs(200 * H + D, 300, H, D, dtype), dtype)
+
+
+@pytest.mark.parametrize("H,D,dtype", CASES)
+def test_larger_graph(H, D, dtype):
+    g = larger_graph(H + D, H, D, dtype)
+    x = inputs(300 * H + D, g[0].size - 1, H, D, dtype, g)
+    check_fwd(x, dtype)
+    check_bwd(x, dtype)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
