@@ -27,7 +27,10 @@ reverse Cuthill-McKee node orders, plus the attention forward under each
 order) and prints one JSON line per measurement; ``--ablate-degree`` times the
 attention forward under the degree-aware partition and two degree-agnostic
 mappings (one lane group per row; one wavefront per row); ``--hd-sweep``
-times the forward over the paper's (H, D) grid on one graph.
+times the forward over the paper's (H, D) grid on one graph; ``--layer`` times
+one of the operators around the attention (differential attention, rotary
+positions, layer norm, each with its backward) on the workload's graph and
+features.
 """
 from __future__ import annotations
 
@@ -433,6 +436,91 @@ def run_backward(args, w, gt, torch, to_device, synth) -> dict:
     return rec
 
 
+LAYER_OPS = ("diff", "diff-backward", "rope", "layernorm", "layernorm-backward")
+
+
+def layer_model_bytes(op: str, N: int, E: int, H: int, D: int, eb: int) -> int:
+    """Bytes of one call by the per-edge model (every gathered row charged) of
+    the attention operators, and read and written once for the others."""
+    row = H * D * eb
+    csr = 8 * (N + 1) + 4 * E
+    return {"diff": csr + 2 * N * row + 2 * E * row,
+            "diff-backward": 2 * csr + 7 * N * row + 4 * E * row + 4 * N * H + 16 * N * H,
+            "rope": 4 * N + 4 * N * row,
+            "layernorm": 2 * N * row + 8 * N + 8 * H * D,
+            "layernorm-backward": 3 * N * row + 8 * N + 12 * H * D}[op]
+
+
+def run_layer(args, w, gt, torch, to_device, synth) -> dict:
+    """One operator around the attention on the workload's features: H heads as
+    H / 2 pairs of maps (differential attention), one axis over the whole head
+    (rotary positions, queries and keys), rows of H * D elements (layer norm)."""
+    op, N, H, D = args.layer, w.N, w.H, w.D
+    if op.startswith("diff") and H % 2:
+        raise SystemExit("--layer %s takes the heads in pairs: a workload of an even number of heads" % op)
+    q, k, v = (to_device(x) for x in (w.Q, w.K, w.V))
+    dev = q.device
+    f32 = dict(dtype=torch.float32, device=dev)
+    if op.startswith("diff"):
+        rp, ci = to_device(w.rowptr), to_device(w.colidx)
+        v = v.view(N, H // 2, 2 * D)
+        lam, out, lse = torch.linspace(0.2, 0.8, H // 2, **f32), torch.empty_like(v), torch.empty((N, H), **f32)
+
+        def step():
+            gt.gt_diff_attn_fwd(rp, ci, q, k, v, lam, out, w.scale, lse=lse)
+
+        if op == "diff-backward":
+            step()
+            rt, ct = (to_device(x) for x in synth.transpose_csr(w.rowptr, w.colidx, N))
+            do = to_device(synth.features(1, N, H, D, w.dtype)[0]).view(v.shape)
+            dq, dk, dv, dl = (torch.empty_like(x) for x in (q, k, v, lam))
+
+            def step():
+                gt.gt_diff_attn_bwd(rp, ci, rt, ct, q, k, v, lam, do, lse, dq, dk, dv, dl, w.scale)
+    elif op == "rope":
+        pos, oq, ok = torch.arange(N, **f32).view(N, 1), torch.empty_like(q), torch.empty_like(k)
+
+        def step():
+            gt.gt_rope(pos, q, oq, [D], K=k, out_k=ok)
+    else:
+        x, do, out = q.view(N, H * D), k.view(N, H * D), torch.empty_like(q).view(N, H * D)
+        gamma, beta, dg, db = (torch.ones(H * D, **f32) for _ in range(4))
+        mean, rstd = torch.empty(N, **f32), torch.empty(N, **f32)
+
+        def step():
+            gt.gt_layernorm_fwd(x, gamma, beta, out, mean=mean, rstd=rstd)
+
+        if op == "layernorm-backward":
+            step()
+
+            def step():
+                gt.gt_layernorm_bwd(x, do, gamma, mean, rstd, out, dgamma=dg, dbeta=db)
+
+    for _ in range(args.warmup):
+        step()
+    ev0, ev1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    torch.cuda.synchronize()
+    ev0.record()
+    for _ in range(args.steps):
+        step()
+    ev1.record()
+    torch.cuda.synchronize()
+    ms = ev0.elapsed_time(ev1) / args.steps
+    mbytes = layer_model_bytes(op, N, w.E, H, D, 4 if w.dtype == "f32" else 2)
+    achieved = mbytes / (ms * 1e-3) / 1e9
+    edges = op.startswith("diff")
+    return {
+        "metric": "%s %s at 1 MI355X; achieved HBM GB/s vs peak" % (op, "GEdges/s" if edges else "GNodes/s"),
+        "value": round((w.E if edges else N) / (ms * 1e-3) / 1e9, 4), "unit": "GEdges/s" if edges else "GNodes/s",
+        "n_gpus": 1, "steps": args.steps, "warmup": args.warmup, "ms_per_step": round(ms, 5),
+        "higher_is_better": True, "scaling": "weak", "vs_baseline": None, "dtype": w.dtype, "data": "synthetic",
+        "config": dict(w.describe(), layer=op),
+        "roofline": {"bound": "hbm", "achieved": round(achieved, 1), "peak": HBM_PEAK_GBPS, "unit": "GB/s",
+                     "frac": round(achieved / HBM_PEAK_GBPS, 4), "algorithmic_bytes_per_launch": mbytes,
+                     "kernel_ms": round(ms, 5)},
+    }
+
+
 def source_hash() -> str:
     """Hash of the library's HIP sources (the .hip file and the headers it
     includes, in name order): counter readings are tied to this."""
@@ -599,6 +687,8 @@ def main() -> int:
                     help="time the GATv2 forward (gt_gatv2_fwd) on the same graph")
     ap.add_argument("--reduce", choices=["min", "max"], default=None,
                     help="time the segment min/max aggregation (gt_segment_reduce)")
+    ap.add_argument("--layer", choices=LAYER_OPS, default=None,
+                    help="time an operator around the attention on the workload's graph and features")
     ap.add_argument("--features", type=int, default=512,
                     help="features per node for --reduce (fp32; default 512)")
     ap.add_argument("--study-reorder", action="store_true",
@@ -654,6 +744,9 @@ def main() -> int:
         return 0
     if args.reduce:
         print(json.dumps(run_reduce(args, w, gt, torch, to_device, synth)), flush=True)
+        return 0
+    if args.layer:
+        print(json.dumps(run_layer(args, w, gt, torch, to_device, synth)), flush=True)
         return 0
     dev = [to_device(x) for x in (w.rowptr, w.colidx, w.Q, w.K, w.V)]
     out = torch.empty_like(dev[2])

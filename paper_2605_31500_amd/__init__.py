@@ -8,6 +8,7 @@ if the library is missing or the call fails, an exception is raised.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -463,16 +464,90 @@ def gt_layernorm_bwd(X, dout, gamma, mean, rstd, dX, dgamma=None, dbeta=None, st
 
 
 def attention(rowptr, colidx, Q, K, V, scale=None, tuning=None, out=None, stream=None,
-              return_lse=False):
+              return_lse=False, pos=None, dims=None, theta=10000.0, layout="pairs"):
     """Convenience: allocates ``out`` like Q (and ``lse`` when asked) and
-    dispatches on Q's dtype."""
+    dispatches on Q's dtype.  With ``pos`` (float32 [N, axes]) the queries and
+    keys are turned by their nodes' positions first (gt_rope; ``dims``:
+    elements of each axis, one axis over the whole head by default)."""
     if out is None:
         out = torch.empty_like(Q)
     if scale is None:
         scale = Q.shape[-1] ** -0.5
+    if pos is not None:
+        Q, K = _turned(pos, Q, K, dims, theta, layout, stream)
     lse = torch.empty(Q.shape[:2], dtype=torch.float32, device=Q.device) if return_lse else None
     gt_attn_fwd_ex(rowptr, colidx, Q, K, V, out, scale, tuning=tuning, stream=stream, lse=lse)
     return (out, lse) if return_lse else out
+
+
+def _on_stream(stream, device):
+    """What a convenience allocates for itself belongs to the stream it is used on."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(stream), device)
+    return torch.cuda.stream(stream)
+
+
+def _turned(pos, Q, K, dims, theta, layout, stream):
+    with _on_stream(stream, Q.device):
+        q, k = torch.empty_like(Q), torch.empty_like(K)
+    gt_rope(pos, Q, q, [Q.shape[-1]] if dims is None else dims, K=K, out_k=k, theta=theta, layout=layout, stream=stream)
+    return q, k
+
+
+def diff_attention(rowptr, colidx, Q, K, V, lam, scale=None, pos=None, dims=None, theta=10000.0, layout="pairs",
+                   norm=None, eps=1e-5, tuning=None, stream=None, return_saved=False):
+    """Convenience: a differential attention block.  Q, K: [N, 2H, D], V: [N, H, 2D], lam: float32 [H].  With ``pos``
+    the queries and keys are turned by their nodes' positions first (as in attention); with ``norm`` = (gamma, beta)
+    (float32 [2D] or None each) every head's output is normalised (layer norm over its 2D elements).  Returns the
+    output [N, H, 2D], and with ``return_saved`` also what diff_attention_bwd needs of the call."""
+    if scale is None:
+        scale = Q.shape[-1] ** -0.5
+    if pos is not None:
+        Q, K = _turned(pos, Q, K, dims, theta, layout, stream)
+    N, H = V.shape[0], V.shape[1]
+    with _on_stream(stream, V.device):
+        out = torch.empty_like(V)
+        lse = torch.empty((N, 2 * H), dtype=torch.float32, device=V.device) if return_saved else None
+    gt_diff_attn_fwd(rowptr, colidx, Q, K, V, lam, out, scale, tuning=tuning, stream=stream, lse=lse)
+    saved = {"Q": Q, "K": K, "V": V, "lam": lam, "scale": scale, "lse": lse, "pos": pos, "dims": dims, "theta": theta,
+             "layout": layout, "norm": norm}
+    if norm is not None:
+        rows = out.view(N * H, V.shape[2])
+        mean = rstd = None
+        with _on_stream(stream, V.device):
+            y = torch.empty_like(rows)
+            if return_saved:
+                mean, rstd = (torch.empty(N * H, dtype=torch.float32, device=V.device) for _ in range(2))
+        gt_layernorm_fwd(rows, norm[0], norm[1], y, eps, mean=mean, rstd=rstd, stream=stream)
+        saved.update(rows=rows, mean=mean, rstd=rstd)
+        out = y.view(V.shape)
+    return (out, saved) if return_saved else out
+
+
+def diff_attention_bwd(rowptr, colidx, rowptr_t, colidx_t, saved, dout, stream=None) -> dict:
+    """Gradients of sum(out * dout) of diff_attention, from its ``saved``: a dict of dQ, dK, dV and dlam, and with a
+    norm also dgamma and dbeta (None where there is no parameter)."""
+    Q, K, V = saved["Q"], saved["K"], saved["V"]
+    grads = {}
+    if saved["norm"] is not None:
+        rows, (gamma, beta) = saved["rows"], saved["norm"]
+        with _on_stream(stream, V.device):
+            drows = torch.empty_like(rows)
+            dgamma, dbeta = (None if p is None else torch.empty_like(p) for p in (gamma, beta))
+        gt_layernorm_bwd(rows, dout.view(rows.shape), gamma, saved["mean"], saved["rstd"], drows, dgamma=dgamma,
+                         dbeta=dbeta, stream=stream)
+        dout = drows.view(V.shape)
+        grads.update(dgamma=dgamma, dbeta=dbeta)
+    with _on_stream(stream, V.device):
+        dQ, dK, dV, dlam = (torch.empty_like(x) for x in (Q, K, V, saved["lam"]))
+    gt_diff_attn_bwd(rowptr, colidx, rowptr_t, colidx_t, Q, K, V, saved["lam"], dout, saved["lse"], dQ, dK, dV, dlam,
+                     saved["scale"], stream=stream)
+    if saved["pos"] is not None:  # (the gradient of a turn is the turn back, in place)
+        gt_rope(saved["pos"], dQ, dQ, [Q.shape[-1]] if saved["dims"] is None else saved["dims"], K=dK, out_k=dK,
+                theta=saved["theta"], layout=saved["layout"], inverse=True, stream=stream)
+    return dict(grads, dQ=dQ, dK=dK, dV=dV, dlam=dlam)
 
 
 def from_numpy(a):

@@ -87,3 +87,11 @@ def test_rope_by_hand():
     assert np.allclose(y[0, 0], want, atol=1e-6)
     y, _ = ref.rope(pos, x[..., [0, 2, 1, 3]], [4], 100.0, "halves", False)
     assert np.allclose(y[0, 0][[0, 2, 1, 3]], want, atol=1e-6)
+
+
+def test_bench_byte_models():
+    import bench
+    # every gathered row of 2HD elements charged; the others read and written once
+    assert bench.layer_model_bytes("diff", 10, 40, 4, 32, 4) == 8 * 11 + 4 * 40 + 2 * 10 * 512 + 2 * 40 * 512
+    assert bench.layer_model_bytes("rope", 10, 40, 4, 32, 2) == 40 + 4 * 10 * 256
+    assert bench.layer_model_bytes("layernorm", 10, 40, 4, 32, 2) == 2 * 10 * 256 + 80 + 8 * 128
