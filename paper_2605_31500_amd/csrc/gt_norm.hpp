@@ -29,29 +29,49 @@ struct NormArgs {
 
 constexpr int32_t kNormMaxF = 16384;
 
-// A row is read once, into registers, by G lanes with K accesses of 16 bytes (W
-// elements) each.  Rows that are no whole number of 16 bytes (ODD) start inside
-// one: `phase` elements of the row before it are read along and masked, and the
-// first and last access of a row store single elements.  A group's rows are all
-// of one phase, so that its accesses hold the same columns in every row.
-typedef uint32_t NormVec __attribute__((ext_vector_type(4)));
+// A row is read once, into registers, by G lanes with K accesses of W elements
+// each: 16 bytes where rows are a whole number of them (NORM_WHOLE), else 4 bytes
+// (NORM_WORDS).  Rows of an odd number of bf16 elements (NORM_PHASE) are read in
+// 16-byte accesses all the same: a row starts inside one, `phase` elements of the
+// row before it are read along and masked, and its first and last access store
+// single elements; a group's rows are all of one phase, so that its accesses hold
+// the same columns in every row.  (fp32 and even bf16 rows by phases / by words,
+// us, forward and backward: 309 K rows of 818 bf16 441 / 210, 522 / 311; 11 K of 3121
+// fp32 58 / 49, 157 / 90.  100 K rows of 819 bf16 by phases: forward 145 with a
+// wavefront for a row and 107 with four, backward 177 and 221.)
+enum { NORM_WHOLE, NORM_WORDS, NORM_PHASE };
 
-template <typename T, int G_, int K_, bool ODD>
+template <int BYTES> struct NormAccess;
+template <> struct NormAccess<16> { typedef uint32_t type __attribute__((ext_vector_type(4))); };
+template <> struct NormAccess<4> { typedef uint32_t type; };
+
+template <typename T, int G_, int K_, int MODE>
 struct NormRow {
-    static constexpr int G = G_, K = K_, W = 16 / Elt<T>::kBytes;
+    static_assert(MODE != NORM_PHASE || std::is_same<T, bf16_tag>::value, "fp32 rows are whole words");
+    static constexpr bool kPhase = MODE == NORM_PHASE;
+    static constexpr int kBytes = MODE == NORM_WORDS ? 4 : 16;
+    static constexpr int G = G_, K = K_, W = kBytes / Elt<T>::kBytes, kDwords = kBytes / 4;
     static constexpr int kThreads = G > kBlock ? G : kBlock;
     static constexpr int kGroups = kThreads / G;  // of a workgroup
-    static constexpr int kAhead = G > kWave || K > 2 ? 1 : 4 / K;  // rows that a group requests together
-    static constexpr int kAheadBwd = K * W > 8 ? 1 : ODD ? (kAhead + 1) / 2 : kAhead;
+    // rows that a group requests together
+    static constexpr int kAhead = G > kWave ? 1 : MODE == NORM_WORDS ? (K <= 4 ? 4 : 2) : K > 2 ? 1 : 4 / K;
+    static constexpr int kAheadBwd = K * W > 8 ? 1 : kPhase ? (kAhead + 1) / 2 : kAhead;
     // parameters stay in registers (read again for every row, us: backward of 60 K rows of
     // 1000 bf16 113 against 77)
-    static constexpr bool kKeep = K * W <= (ODD ? 16 : 32);
-    NormVec v[K];
+    static constexpr bool kKeep = K * W <= (kPhase ? 16 : 32);
+    typedef typename NormAccess<kBytes>::type Vec;
+    Vec v[K];
 
     // Column of the first element of access k.
-    __device__ __forceinline__ static int column(int lig, int k, int phase) { return (lig + k * G) * W - (ODD ? phase : 0); }
+    __device__ __forceinline__ static int column(int lig, int k, int phase) { return (lig + k * G) * W - (kPhase ? phase : 0); }
     __device__ __forceinline__ static bool holds(int col, int e, int32_t F) {
-        return ODD ? (uint32_t)(col + e) < (uint32_t)F : col < F;
+        return kPhase ? (uint32_t)(col + e) < (uint32_t)F : col < F;
+    }
+    __device__ __forceinline__ static uint32_t dword(const Vec& x, int d) {
+        if constexpr (kDwords == 1)
+            return x;
+        else
+            return x[d];
     }
 
     // (elements of other rows are read as 0)
@@ -62,65 +82,65 @@ struct NormRow {
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int c = column(lig, k, phase);
-            v[k] = NormVec{0, 0, 0, 0};
-            if (c >= F || (ODD && c + W <= 0)) continue;
-            if (ODD && c + W > left) {  // (nothing past the end)
+            v[k] = Vec{};
+            if (c >= F || (kPhase && c + W <= 0)) continue;
+            const Vec* at = reinterpret_cast<const Vec*>(p + c);
+            if constexpr (kPhase) {
+                uint32_t mask[kDwords];
 #pragma unroll
-                for (int e = 0; e < W; ++e) {
-                    if (!holds(c, e, F)) continue;
-                    if constexpr (W == 4)
-                        v[k][e] = __float_as_uint(p[c + e]);
-                    else
-                        v[k][e / 2] |= (uint32_t)p[c + e] << (e % 2 * 16);
+                for (int d = 0; d < kDwords; ++d)
+                    mask[d] = (holds(c, 2 * d, F) ? 0x0000FFFFu : 0u) | (holds(c, 2 * d + 1, F) ? 0xFFFF0000u : 0u);
+                if (c + W > left) {  // (nothing past the end)
+#pragma unroll
+                    for (int e = 0; e < W; ++e)
+                        if (holds(c, e, F)) v[k][e / 2] |= (uint32_t)p[c + e] << (e % 2 * 16);
+                } else {
+                    v[k] = *at;
+#pragma unroll
+                    for (int d = 0; d < kDwords; ++d) v[k][d] &= mask[d];
                 }
             } else {
                 // past the caches, unless two rows share lines (plain loads throughout / past
                 // the caches, us: backward of 169 K rows of 512 fp32 194 / 183, of 60 K rows of
                 // 203 bf16 26.0 / 31.0; a choice at run time costs the former 9)
-                const NormVec* at = reinterpret_cast<const NormVec*>(p + c);
-                v[k] = ODD ? *at : __builtin_nontemporal_load(at);
-                if constexpr (ODD) {
-#pragma unroll
-                    for (int d = 0; d < 4; ++d)
-                        if constexpr (W == 4)
-                            v[k][d] = holds(c, d, F) ? v[k][d] : 0u;
-                        else
-                            v[k][d] &= (holds(c, 2 * d, F) ? 0x0000FFFFu : 0u) | (holds(c, 2 * d + 1, F) ? 0xFFFF0000u : 0u);
-                }
+                v[k] = MODE == NORM_WHOLE ? __builtin_nontemporal_load(at) : *at;
             }
         }
     }
 
     __device__ __forceinline__ void elements(int k, float (&x)[W]) const {
-        widen<T>(make_uint4(v[k][0], v[k][1], v[k][2], v[k][3]), x);
+#pragma unroll
+        for (int e = 0; e < W; ++e)
+            if constexpr (std::is_same<T, float>::value)
+                x[e] = __uint_as_float(dword(v[k], e));
+            else
+                x[e] = __uint_as_float(e % 2 ? dword(v[k], e / 2) & 0xFFFF0000u : dword(v[k], e / 2) << 16);
     }
 
     __device__ __forceinline__ static void store(void* base, int64_t row, int32_t F, int lig, int phase, int k, const float (&x)[W]) {
         typedef typename Raw<T>::type R;
         R* p = static_cast<R*>(base) + row * F;
         const int c = column(lig, k, phase);
-        if (c >= F || (ODD && c + W <= 0)) return;
-        NormVec o;
+        if (c >= F || (kPhase && c + W <= 0)) return;
+        uint32_t o[kDwords];
 #pragma unroll
-        for (int d = 0; d < 4; ++d)
-            if constexpr (W == 4)
+        for (int d = 0; d < kDwords; ++d)
+            if constexpr (std::is_same<T, float>::value)
                 o[d] = __float_as_uint(x[d]);
             else
                 o[d] = pack_bf16(x[2 * d], x[2 * d + 1]);
-        if (ODD && (c < 0 || c + W > F)) {
+        Vec y;
+        __builtin_memcpy(&y, o, sizeof y);
+        Vec* at = reinterpret_cast<Vec*>(p + c);
+        if constexpr (MODE == NORM_WHOLE) {
+            __builtin_nontemporal_store(y, at);
+        } else {  // (rows share lines: left to the L2 to put together)
+            if (!kPhase || (c >= 0 && c + W <= F))
+                *at = y;
+            else
 #pragma unroll
-            for (int e = 0; e < W; ++e)
-                if (holds(c, e, F)) {
-                    if constexpr (W == 4)
-                        p[c + e] = x[e];
-                    else
-                        p[c + e] = (R)(o[e / 2] >> (e % 2 * 16));
-                }
-        } else if constexpr (ODD) {
-            // (rows share lines: left to the L2 to put together)
-            *reinterpret_cast<NormVec*>(p + c) = o;
-        } else {
-            __builtin_nontemporal_store(o, reinterpret_cast<NormVec*>(p + c));
+                for (int e = 0; e < W; ++e)
+                    if (holds(c, e, F)) p[c + e] = (R)(o[e / 2] >> (e % 2 * 16));
         }
     }
 
@@ -134,19 +154,19 @@ struct NormRow {
 
 // The rows of a group: `first` and every `step` after it, and with each of them
 // the next ones `apart`.  A workgroup's rows follow one another, unless those of
-// a group would be of different phases then (ODD: the grid is a multiple of 8).
+// a group would be of different phases then (the grid is a multiple of 8).
 // (Rows that a group requests together apart by the grid, fp32 and bf16 alike:
 // 1 M rows of 256 bf16 elements 214 us against 198.)
-template <typename Row, bool ODD, int AHEAD>
+template <typename Row, int AHEAD>
 struct NormRows {
-    static constexpr bool kTogether = !ODD || Row::kGroups % Row::W == 0;
+    static constexpr bool kTogether = !Row::kPhase || Row::kGroups % Row::W == 0;
     int64_t first, step, apart;
     int phase;
     __device__ __forceinline__ NormRows(int32_t F, int g) {
         first = (int64_t)blockIdx.x * Row::kGroups * (kTogether ? AHEAD : 1) + g;
         step = (int64_t)gridDim.x * Row::kGroups * AHEAD;
         apart = kTogether ? Row::kGroups : (int64_t)gridDim.x * Row::kGroups;
-        phase = ODD ? (int)((first % Row::W) * (F % Row::W) % Row::W) : 0;
+        phase = Row::kPhase ? (int)((first % Row::W) * (F % Row::W) % Row::W) : 0;
     }
 };
 
@@ -176,16 +196,16 @@ __device__ __forceinline__ void group_sum(float (&x)[M], float* lds, int& turn) 
     }
 }
 
-template <typename T, int G, int K, bool ODD>
-__global__ void __launch_bounds__((NormRow<T, G, K, ODD>::kThreads)) gt_norm_fwd_kernel(NormArgs a) {
-    using Row = NormRow<T, G, K, ODD>;
+template <typename T, int G, int K, int MODE>
+__global__ void __launch_bounds__((NormRow<T, G, K, MODE>::kThreads)) gt_norm_fwd_kernel(NormArgs a) {
+    using Row = NormRow<T, G, K, MODE>;
     constexpr int W = Row::W;
     constexpr int kAhead = Row::kAhead;
     __shared__ float lds[G > kWave ? 2 * G / kWave : 1];
     int turn = 0;
     const int lig = threadIdx.x % G, g = threadIdx.x / G;
     const float inv_f = 1.0f / (float)a.F;
-    const NormRows<Row, ODD, kAhead> rows(a.F, g);
+    const NormRows<Row, kAhead> rows(a.F, g);
     constexpr bool kKeep = Row::kKeep;
     float gm[kKeep ? K : 1][W], bt[kKeep ? K : 1][W];
     if constexpr (kKeep)
@@ -252,9 +272,9 @@ __global__ void __launch_bounds__((NormRow<T, G, K, ODD>::kThreads)) gt_norm_fwd
 // Backward.  A group sums its rows' shares of the parameters' gradients in
 // registers; at the end they are added over the groups of the workgroup, which
 // leaves one partial row each of dgamma and dbeta in `part` [workgroup][2][F].
-template <typename T, int G, int K, bool ODD>
-__global__ void __launch_bounds__((NormRow<T, G, K, ODD>::kThreads)) gt_norm_bwd_kernel(NormArgs a, float* part) {
-    using Row = NormRow<T, G, K, ODD>;
+template <typename T, int G, int K, int MODE>
+__global__ void __launch_bounds__((NormRow<T, G, K, MODE>::kThreads)) gt_norm_bwd_kernel(NormArgs a, float* part) {
+    using Row = NormRow<T, G, K, MODE>;
     constexpr int W = Row::W;
     constexpr int kAhead = Row::kAheadBwd;
     constexpr int kLdsSum = G > kWave ? 4 * G / kWave : 0, kLdsParam = Row::kGroups > 1 ? Row::kThreads * K * W : 0;
@@ -267,7 +287,7 @@ __global__ void __launch_bounds__((NormRow<T, G, K, ODD>::kThreads)) gt_norm_bwd
     for (int k = 0; k < K; ++k)
 #pragma unroll
         for (int i = 0; i < W; ++i) sg[k][i] = sb[k][i] = 0.0f;
-    const NormRows<Row, ODD, kAhead> rows(a.F, g);
+    const NormRows<Row, kAhead> rows(a.F, g);
     constexpr bool kKeep = Row::kKeep;
     float gm[kKeep ? K : 1][W];
     if constexpr (kKeep)
@@ -388,39 +408,39 @@ gt_norm_param_kernel(const float* part, int blocks, int32_t F, float* dgamma, fl
 
 // Workgroups: all that the device holds at once (each keeps its parameters and
 // sums for many rows), or one for the rows that its groups request together.
-template <typename T, int G, int K, bool ODD, bool BACKWARD>
+template <typename T, int G, int K, int MODE, bool BACKWARD>
 int norm_blocks(int64_t rows_per_block, int64_t N, int dev) {
     static std::atomic<int> cache[64];
     int most = dev >= 0 && dev < 64 ? cache[dev].load() : 0;
     if (most == 0) {
         int nb = 0;
-        const void* kernel = BACKWARD ? reinterpret_cast<const void*>(gt_norm_bwd_kernel<T, G, K, ODD>)
-                                      : reinterpret_cast<const void*>(gt_norm_fwd_kernel<T, G, K, ODD>);
-        if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&nb, kernel, NormRow<T, G, K, ODD>::kThreads, 0) != hipSuccess || nb <= 0) nb = 1;
+        const void* kernel = BACKWARD ? reinterpret_cast<const void*>(gt_norm_bwd_kernel<T, G, K, MODE>)
+                                      : reinterpret_cast<const void*>(gt_norm_fwd_kernel<T, G, K, MODE>);
+        if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&nb, kernel, NormRow<T, G, K, MODE>::kThreads, 0) != hipSuccess || nb <= 0) nb = 1;
         most = nb * device_cus(dev);
         if (dev >= 0 && dev < 64) cache[dev] = most;
     }
     int64_t need = (N + rows_per_block - 1) / rows_per_block;
     if (need > most) need = most;
-    return (int)(ODD ? (need + 7) / 8 * 8 : need);
+    return (int)(MODE == NORM_PHASE ? (need + 7) / 8 * 8 : need);
 }
 
-template <typename T, int G, int K, bool ODD>
+template <typename T, int G, int K, int MODE>
 gt_status launch_norm(const NormArgs& a, bool backward, int dev, hipStream_t stream) {
-    using Row = NormRow<T, G, K, ODD>;
+    using Row = NormRow<T, G, K, MODE>;
     hipError_t he = hipSuccess;
     if (!backward) {
-        const int blocks = norm_blocks<T, G, K, ODD, false>(Row::kGroups * Row::kAhead, a.N, dev);
-        hipLaunchKernelGGL((gt_norm_fwd_kernel<T, G, K, ODD>), dim3(blocks), dim3(Row::kThreads), 0, stream, a);
+        const int blocks = norm_blocks<T, G, K, MODE, false>(Row::kGroups * Row::kAhead, a.N, dev);
+        hipLaunchKernelGGL((gt_norm_fwd_kernel<T, G, K, MODE>), dim3(blocks), dim3(Row::kThreads), 0, stream, a);
         he = hipGetLastError();
         return he == hipSuccess ? GT_SUCCESS : hip_fail(he, "layer norm launch");
     }
-    const int blocks = norm_blocks<T, G, K, ODD, true>(Row::kGroups * Row::kAheadBwd, a.N, dev);
+    const int blocks = norm_blocks<T, G, K, MODE, true>(Row::kGroups * Row::kAheadBwd, a.N, dev);
     CallWorkspace cw;
     if (a.dgamma || a.dbeta)
         if (const gt_status st = acquire_workspace(dev, (size_t)blocks * 2 * a.F * sizeof(float), stream, cw); st != GT_SUCCESS) return st;
     float* part = reinterpret_cast<float*>(cw.ptr);
-    hipLaunchKernelGGL((gt_norm_bwd_kernel<T, G, K, ODD>), dim3(blocks), dim3(Row::kThreads), 0, stream, a, part);
+    hipLaunchKernelGGL((gt_norm_bwd_kernel<T, G, K, MODE>), dim3(blocks), dim3(Row::kThreads), 0, stream, a, part);
     if ((he = hipGetLastError()) != hipSuccess) return hip_fail(he, "layer norm backward launch");
     if (part) {
         hipLaunchKernelGGL(gt_norm_param_kernel, dim3((2 * a.F + kNormCols - 1) / kNormCols), dim3(kNormCols * kNormStretches), 0, stream, part, blocks, a.F,
@@ -430,25 +450,60 @@ gt_status launch_norm(const NormArgs& a, bool backward, int dev, hipStream_t str
     return GT_SUCCESS;
 }
 
-// The lanes of a row by its accesses (ODD: with those of the largest phase).  A
-// wavefront takes rows of up to four accesses per lane, since a row of more
-// wavefronts waits for their sums; masks cost ODD rows more registers, which get
-// more lanes instead.
-template <typename T, bool ODD>
-gt_status pick_norm(const NormArgs& a, bool backward, int dev, hipStream_t stream) {
-    constexpr int W = 16 / Elt<T>::kBytes;
-    const int32_t c = (a.F + (ODD ? W - 1 : 0) + W - 1) / W;
-    if (c <= 8) return launch_norm<T, 8, 1, ODD>(a, backward, dev, stream);
-    if (c <= 16) return launch_norm<T, 16, 1, ODD>(a, backward, dev, stream);
-    if (c <= 32) return launch_norm<T, 32, 1, ODD>(a, backward, dev, stream);
-    if (c <= 64) return launch_norm<T, 64, 1, ODD>(a, backward, dev, stream);
-    if (c <= 128) return launch_norm<T, 64, 2, ODD>(a, backward, dev, stream);
-    if (c <= 256) return launch_norm<T, ODD ? 256 : 64, ODD ? 1 : 4, ODD>(a, backward, dev, stream);
-    if (c <= 512) return launch_norm<T, 256, 2, ODD>(a, backward, dev, stream);
-    if (c <= 1024) return launch_norm<T, ODD ? 512 : 256, ODD ? 2 : 4, ODD>(a, backward, dev, stream);
-    if (c <= 2048) return launch_norm<T, ODD ? 1024 : 512, ODD ? 2 : 4, ODD>(a, backward, dev, stream);
-    if constexpr (W == 4 || ODD) return launch_norm<T, 1024, W == 8 ? 3 : ODD ? 5 : 4, ODD>(a, backward, dev, stream);
-    return GT_ERROR_NOT_SUPPORTED;  // (kNormMaxF)
+// The lanes of a row by its accesses.  A wavefront takes rows of a few accesses
+// per lane, since a row of more wavefronts waits for their sums; the masks of
+// phases cost registers, which get more lanes instead.
+template <typename T>
+gt_status pick_whole(const NormArgs& a, bool backward, int dev, hipStream_t stream) {
+    constexpr int M = NORM_WHOLE;
+    const int32_t c = a.F / NormRow<T, 8, 1, M>::W;
+    if (c <= 4) return launch_norm<T, 4, 1, M>(a, backward, dev, stream);
+    if (c <= 8) return launch_norm<T, 8, 1, M>(a, backward, dev, stream);
+    if (c <= 16) return launch_norm<T, 16, 1, M>(a, backward, dev, stream);
+    if (c <= 32) return launch_norm<T, 32, 1, M>(a, backward, dev, stream);
+    if (c <= 64) return launch_norm<T, 64, 1, M>(a, backward, dev, stream);
+    if (c <= 128) return launch_norm<T, 64, 2, M>(a, backward, dev, stream);
+    if (c <= 256) return launch_norm<T, 64, 4, M>(a, backward, dev, stream);
+    if (c <= 512) return launch_norm<T, 256, 2, M>(a, backward, dev, stream);
+    if (c <= 1024) return launch_norm<T, 256, 4, M>(a, backward, dev, stream);
+    if constexpr (std::is_same<T, float>::value)
+        if (c > 2048) return launch_norm<T, 1024, 4, M>(a, backward, dev, stream);
+    return launch_norm<T, 512, 4, M>(a, backward, dev, stream);
+}
+
+template <typename T>
+gt_status pick_words(const NormArgs& a, bool backward, int dev, hipStream_t stream) {
+    constexpr int M = NORM_WORDS;
+    const int32_t c = a.F / NormRow<T, 8, 1, M>::W;
+    if (c <= 8) return launch_norm<T, 8, 1, M>(a, backward, dev, stream);
+    if (c <= 16) return launch_norm<T, 16, 1, M>(a, backward, dev, stream);
+    if (c <= 32) return launch_norm<T, 32, 1, M>(a, backward, dev, stream);
+    if (c <= 64) return launch_norm<T, 64, 1, M>(a, backward, dev, stream);
+    if (c <= 128) return launch_norm<T, 64, 2, M>(a, backward, dev, stream);
+    if (c <= 256) return launch_norm<T, 64, 4, M>(a, backward, dev, stream);
+    if (c <= 512) return launch_norm<T, 64, 8, M>(a, backward, dev, stream);
+    if (c <= 1024) return launch_norm<T, 256, 4, M>(a, backward, dev, stream);
+    if (c <= 2048) return launch_norm<T, 256, 8, M>(a, backward, dev, stream);
+    if (c <= 4096) return launch_norm<T, 512, 8, M>(a, backward, dev, stream);
+    if constexpr (std::is_same<T, float>::value)
+        if (c > 8192) return launch_norm<T, 1024, 16, M>(a, backward, dev, stream);
+    return launch_norm<T, 1024, 8, M>(a, backward, dev, stream);
+}
+
+gt_status pick_phase(const NormArgs& a, bool backward, int dev, hipStream_t stream) {
+    typedef bf16_tag T;
+    constexpr int M = NORM_PHASE;
+    const int32_t c = (a.F + 14) / 8;  // (with the largest phase)
+    if (c <= 4) return launch_norm<T, 4, 1, M>(a, backward, dev, stream);
+    if (c <= 8) return launch_norm<T, 8, 1, M>(a, backward, dev, stream);
+    if (c <= 16) return launch_norm<T, 16, 1, M>(a, backward, dev, stream);
+    if (c <= 32) return launch_norm<T, 32, 1, M>(a, backward, dev, stream);
+    if (c <= 64) return launch_norm<T, 64, 1, M>(a, backward, dev, stream);
+    if (c <= 128 && backward) return launch_norm<T, 64, 2, M>(a, backward, dev, stream);
+    if (c <= 256) return launch_norm<T, 256, 1, M>(a, backward, dev, stream);
+    if (c <= 512) return launch_norm<T, 512, 1, M>(a, backward, dev, stream);
+    if (c <= 1024) return launch_norm<T, 1024, 1, M>(a, backward, dev, stream);
+    return launch_norm<T, 1024, 3, M>(a, backward, dev, stream);
 }
 
 template <typename T>
@@ -460,7 +515,11 @@ gt_status dispatch_norm(const NormArgs& a, bool backward, int dev, hipStream_t s
                     return hip_fail(he, "layer norm parameter launch");
         return GT_SUCCESS;
     }
-    return a.F % (16 / Elt<T>::kBytes) == 0 ? pick_norm<T, false>(a, backward, dev, stream) : pick_norm<T, true>(a, backward, dev, stream);
+    const int64_t bytes = (int64_t)a.F * Elt<T>::kBytes;
+    if (bytes % 16 == 0) return pick_whole<T>(a, backward, dev, stream);
+    if constexpr (std::is_same<T, bf16_tag>::value)
+        if (bytes % 4 != 0) return pick_phase(a, backward, dev, stream);
+    return pick_words<T>(a, backward, dev, stream);
 }
 
 gt_status run_norm(gt_dtype dtype, const NormArgs& a, bool backward, hipStream_t stream) {
