@@ -228,6 +228,83 @@ __global__ void __launch_bounds__(kBlock) gt_rope_kernel(RopeParams r) {
     }
 }
 
+// Where the pairs do not come in whole accesses but heads are whole 16-byte
+// vectors: a thread keeps one place in a head (W elements) for all rows of a
+// node and head that it takes, and so its elements' partners and frequencies.
+// Rows pass through LDS, from which it reads the partners; they still move by 16
+// bytes (us, by units / so: single bf16 elements, 194 K nodes of 4x128 253 / 180,
+// 241 K of 2x32 54 / 35; two bf16, 524 K of 8x64 532 / 430, but 523 K of 2x32 70 /
+// 80; four bf16, 524 K of 8x64 411 / 430; two fp32, 390 K of 4x128 690 / 630).
+template <typename T>
+__global__ void __launch_bounds__(kBlock) gt_rope_rows_kernel(RopeParams r) {
+    typedef typename Raw<T>::type R;
+    constexpr int W = 16 / Elt<T>::kBytes, kRows = 2;
+    using Unit = RopeUnit<T, W>;
+    typedef typename Unit::Vec Vec;
+    __shared__ float2 table[kRopeTable];
+    __shared__ double freq[kRopeMaxD / 2];
+    __shared__ int32_t axis[kRopeMaxD / 2];
+    __shared__ uint32_t element[kRopeMaxD];  // partner | pair << 10 | turned << 30 | second of its pair << 31
+    __shared__ __attribute__((aligned(16))) R stage[2][kRows * kBlock * W];
+    const int half = r.turned / 2, vecs = r.D / W;
+    for (int x = threadIdx.x; x < r.D; x += kBlock) element[x] = (uint32_t)x;
+    __syncthreads();
+    for (int p = threadIdx.x; p < half; p += kBlock) {
+        const RopePair q = rope_pair(r, p);
+        freq[p] = q.freq;
+        axis[p] = q.axis;
+        element[q.lo] = (uint32_t)q.hi | (uint32_t)p << 10 | 1u << 30;
+        element[q.hi] = (uint32_t)q.lo | (uint32_t)p << 10 | 3u << 30;
+    }
+    __syncthreads();
+    const int at_once = kBlock / vecs, place = threadIdx.x % vecs, mine = threadIdx.x / vecs;  // (vecs <= 128)
+    const bool idle = mine >= at_once;
+    uint32_t el[W];
+#pragma unroll
+    for (int e = 0; e < W; ++e) el[e] = element[place * W + e];
+    const Quotient by_half(half), by_heads(r.H);
+    for (int64_t n0 = (int64_t)blockIdx.x * r.nodes; n0 < r.N; n0 += (int64_t)gridDim.x * r.nodes) {
+        const int nodes = (int)(r.N - n0 < r.nodes ? r.N - n0 : r.nodes);
+        __syncthreads();
+        for (int i = threadIdx.x; i < nodes * half; i += kBlock) {
+            const int n = by_half(i), p = i - n * half;
+            float2 cs = rope_cos_sin((double)r.pos[(n0 + n) * r.axes + axis[p]] * freq[p]);
+            cs.y *= r.sign;
+            table[i] = cs;
+        }
+        const int each = nodes * r.H, total = (r.K ? 2 : 1) * each;
+        const int64_t row0 = n0 * r.H;
+        for (int i0 = 0, turn = 0; i0 < total; i0 += kRows * at_once, turn ^= 1) {
+            Vec v[kRows];
+#pragma unroll
+            for (int j = 0; j < kRows; ++j) {
+                const int i = i0 + j * at_once + mine, k = i >= each ? i - each : i;
+                if (idle || i >= total) continue;
+                v[j] = *reinterpret_cast<const Vec*>(static_cast<const R*>(i >= each ? r.K : r.Q) + (row0 + k) * r.D + place * W);
+                *reinterpret_cast<Vec*>(&stage[turn][(j * at_once + mine) * r.D + place * W]) = v[j];
+            }
+            __syncthreads();  // (rows and table are there; the other stage's readers are past the sync before)
+#pragma unroll
+            for (int j = 0; j < kRows; ++j) {
+                const int i = i0 + j * at_once + mine, k = i >= each ? i - each : i;
+                if (idle || i >= total) continue;
+                const R* row = &stage[turn][(j * at_once + mine) * r.D];
+                const float2* cs = table + by_heads(k) * half;
+                float x[W], o[W];
+                Unit::widen_to(v[j], x);
+#pragma unroll
+                for (int e = 0; e < W; ++e) {
+                    const float y = to_f32(row[el[e] & 1023u]);
+                    const float2 c = cs[(el[e] >> 10) & 1023u];
+                    const float turned = el[e] >> 31 ? y * c.y + x[e] * c.x : x[e] * c.x - y * c.y;
+                    o[e] = el[e] >> 30 & 1u ? turned : x[e];
+                }
+                *reinterpret_cast<Vec*>(static_cast<R*>(i >= each ? r.outK : r.outQ) + (row0 + k) * r.D + place * W) = Unit::narrow_from(o);
+            }
+        }
+    }
+}
+
 // Elements of an access: the most, up to 16 bytes, that divide every stretch of
 // elements which lie together with their partners, and the rest of the head.
 int rope_access(const RopeParams& r, int elt_bytes) {
@@ -263,10 +340,25 @@ gt_status launch_rope(RopeParams r, int dev, hipStream_t stream) {
     return he == hipSuccess ? GT_SUCCESS : hip_fail(he, "rotary launch");
 }
 
+// Units of fewer elements than this leave their rows to gt_rope_rows_kernel.
+constexpr int kRopeRowsBelow = 4;
+
+template <typename T>
+gt_status launch_rope_rows(RopeParams r, int dev, hipStream_t stream) {
+    const int64_t most = kRopeTable / (r.turned / 2), even = (r.N + 4 * device_cus(dev) - 1) / (4 * device_cus(dev));
+    const int64_t held = kRopeHeld / r.H;  // (node and head rows below 2^16)
+    r.nodes = (int32_t)std::min(std::min(even, most), held);
+    const int64_t blocks = std::min<int64_t>((r.N + r.nodes - 1) / r.nodes, 8 * device_cus(dev));
+    hipLaunchKernelGGL(gt_rope_rows_kernel<T>, dim3((unsigned)blocks), dim3(kBlock), 0, stream, r);
+    const hipError_t he = hipGetLastError();
+    return he == hipSuccess ? GT_SUCCESS : hip_fail(he, "rotary launch");
+}
+
 template <typename T>
 gt_status pick_rope(const RopeParams& r, int dev, hipStream_t stream) {
     constexpr int kMost = 16 / Elt<T>::kBytes;
     const int w = rope_access(r, Elt<T>::kBytes);
+    if (w < kRopeRowsBelow && r.D % kMost == 0) return launch_rope_rows<T>(r, dev, stream);
     if (r.layout == GT_ROPE_PAIRS) {  // (w is even: so are the sections)
         if constexpr (kMost == 8)
             if (w == 8) return launch_rope<T, 8, true>(r, dev, stream);
