@@ -34,10 +34,11 @@ extern "C" {
  *
  * Layouts: Q, K [N][2H][D]; V, out [N][H][2D], in `dtype`, 16-byte aligned;
  * lambda float [H], any values; lse (may be NULL) float [N][2H], receives
- * ln(sum_e exp(s_m,e)).  An entry whose score is -inf has weight 0; a row
- * without entries, or with none but such, counts as empty in that map: the
- * map's sum is 0 and its lse -inf.  Inf and NaN in the K or V row of a node
- * reach only the rows whose entries name that node.
+ * ln(sum_e exp(s_m,e)).  An entry whose score is -inf has weight 0 (its
+ * value row still enters, times 0); a row without entries, or with none but
+ * such, counts as empty in that map: the map's sum is 0 and its lse -inf.  Inf
+ * and NaN in the K or V row of a node reach only the rows whose entries name
+ * that node.
  * Supported shapes: H in {1, 2, 4, 8} with D in {32, 64, 128}, and for bf16
  * features also D = 256 (a value head's 2D elements must fit 64 lanes of 16
  * bytes); 0 <= E < 2^31; 0 <= N < 2^31.
@@ -95,8 +96,8 @@ gt_status gt_diff_attn_bwd(gt_dtype dtype, const int64_t* rowptr, const int32_t*
  *                    dims[a] / 2 pairs p after those of the axes before it
  * theta > 0, finite.  The angle is reduced to a part of a turn in 64 bits, so
  * far positions keep their accuracy; the turned values are computed in fp32 and
- * rounded once (bf16: to nearest even).  A node whose position is not finite
- * gets NaN in that axis' elements.  inverse != 0 turns by -t: the inverse, which
+ * rounded once (bf16: to nearest even).  A node whose angle is not finite
+ * (its position is not, or overflows) gets NaN in that axis' elements.  inverse != 0 turns by -t: the inverse, which
  * is also the operator's gradient.
  * Layouts: pos float [N][axes], 4-byte aligned; Q, K, outQ, outK [N][H][D] in
  * `dtype`, 16-byte aligned; K and outK may both be NULL.  outQ may be Q itself
@@ -136,10 +137,11 @@ gt_status gt_rope(gt_dtype dtype, const float* pos, const void* Q, const void* K
  * dgamma, dbeta float [F], each of which may be NULL (gamma: 1, beta: 0,
  * gradients: not wanted); mean, rstd float [N], which the forward writes if they
  * are not NULL and the backward reads.  1 <= F <= 16384, any F (rows of whole
- * 16-byte vectors are read fastest); 0 <= N < 2^31; eps >= 0, finite.  Sums are
- * fp32, the parameters' gradients summed over rows in a fixed order; bf16
- * outputs are rounded to nearest even.  out may be X itself and dX may be X or
- * dout itself; other overlaps are refused.  N == 0 sets dgamma and dbeta to 0.
+ * 16-byte vectors are read fastest); 0 <= N < 2^31; eps >= 0, finite (with
+ * eps = 0 a constant row gives 0 / 0).  Sums are fp32, the parameters' gradients
+ * summed over rows in a fixed order; bf16 outputs are rounded to nearest even.
+ * out may be X itself and dX may be X or dout itself; other overlaps are
+ * refused.  N == 0 sets dgamma and dbeta to 0.
  */
 gt_status gt_layernorm_fwd(gt_dtype dtype, const void* X, const float* gamma, const float* beta, void* out,
                            float* mean, float* rstd, int64_t N, int32_t F, float eps, hipStream_t stream);

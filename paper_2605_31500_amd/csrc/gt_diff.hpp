@@ -10,6 +10,16 @@
 // of its map, and each lane then needs both maps' weights for its value elements:
 // it computes its own map's and takes the other's from the lanes HL away.  The
 // normalisers are known only at a row's end, hence two accumulators per element.
+//
+// Like the other row kernels these gather two random rows per entry and are bound
+// by the path from L2 to the fabric (kernel time; bytes beyond the L2): forward,
+// power law of 169 K nodes fp32 2x32 150 us, 7.1 TB/s; R-MAT of 1 M nodes bf16
+// 2x32 1130 us, 6.7 TB/s, with the vector units busy for two thirds of it;
+// lognormal 200 K nodes bf16 4x64 1600 us, 7.8 TB/s asked for; backward, R-MAT of
+// 500 K nodes bf16 2x32 544 and 665 us, 6.3 and 6.5 TB/s.  Eight entries per step
+// where a wavefront holds four groups (four / eight, us): 1130 / 1180, 544 / 581,
+// 665 / 780.  All coefficients stay in fp32 and multiply exactly widened rows: the
+// one rounding to bf16 is that of the results.
 
 // The other map's value, from the other HL lanes of the pair (every lane of a
 // map holds the same value).
@@ -493,7 +503,11 @@ __global__ void __launch_bounds__(kBlock) gt_diff_kernel(DiffParams p) {
 }
 
 // The partial states of each cut row, merged in a fixed order as in
-// gt_bwd_merge_kernel: one wavefront per row and slice.
+// gt_bwd_merge_kernel: one wavefront per row and slice.  (Two pieces of a lane
+// group in flight; with four the states take 152 registers and a row's eight
+// pieces half of them: R-MAT of 1 M nodes bf16 2x32 57 against 44 us.)
+constexpr uint32_t kDiffMergePieces = 2;
+
 template <typename Op, typename T, int PS, int D>
 __global__ void __launch_bounds__(kBlock) gt_diff_merge_kernel(DiffParams p) {
     constexpr uint32_t G = Op::kG, P = kWave / G;
@@ -510,16 +524,16 @@ __global__ void __launch_bounds__(kBlock) gt_diff_merge_kernel(DiffParams p) {
         const int32_t row = cut.row(p.w, i, lane, slot, nq);
         typename Op::State st;
         st.reset();
-        for (uint32_t q0 = 0; q0 < nq; q0 += P * kMergePieces) {
+        for (uint32_t q0 = 0; q0 < nq; q0 += P * kDiffMergePieces) {
             // (a group without a piece reads the row's last and leaves it out)
-            typename Op::State::Partial pt[kMergePieces];
+            typename Op::State::Partial pt[kDiffMergePieces];
 #pragma unroll
-            for (uint32_t u = 0; u < kMergePieces; ++u) {
+            for (uint32_t u = 0; u < kDiffMergePieces; ++u) {
                 const uint32_t q = q0 + u * P + g;
                 st.load_partial(op, (int32_t)(slot + (q < nq ? q : nq - 1)), lig, pt[u]);
             }
 #pragma unroll
-            for (uint32_t u = 0; u < kMergePieces; ++u) st.add(pt[u], q0 + u * P + g < nq);
+            for (uint32_t u = 0; u < kDiffMergePieces; ++u) st.add(pt[u], q0 + u * P + g < nq);
         }
 #pragma unroll
         for (int off = G; off < kWave; off <<= 1) st.merge_xor(off);
@@ -531,7 +545,9 @@ __global__ void __launch_bounds__(kBlock) gt_diff_merge_kernel(DiffParams p) {
 // lane groups, in id order.  A group reads a row of up to kDirectAlone entries by
 // itself; longer ones are then read one after another by all groups of the
 // workgroup, a share each, and merged in LDS in a fixed order.  One launch takes
-// the place of three (clear and partition, rows, merge).
+// the place of three (clear and partition, rows, merge).  (Rows read alone up to 16
+// / 32 / 64 entries, us: 1.5 K nodes of degree 31, forward 33 / 11.4 / 11.5,
+// backward 64 / 40 / 28; 1.5 K R-MAT nodes, backward 62 / 55 / 61.)
 constexpr uint32_t kDirectAlone = 48;
 
 template <typename Op, typename T, int PS, int D>

@@ -267,3 +267,101 @@ def test_bench_modes():
         assert r.returncode == 0, r.stderr[-2000:]
         line = json.loads(r.stdout.strip().splitlines()[-1])
         assert line["value"] > 0 and line["config"]["layer"] == op and line["roofline"]["frac"] > 0
+
+
+# ------------------------------------------------------- offsets past 32 bits
+
+
+def rows_of_bits(n, width, seed):
+    """bf16 rows [n, width] made on the device, of more than 2^32 bytes."""
+    import torch
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    x = torch.empty((n, width), dtype=torch.bfloat16, device="cuda")
+    step = 1 << 17
+    for a in range(0, n, step):
+        x[a:a + step] = torch.randn((min(step, n - a), width), generator=g, device="cuda")
+    return x
+
+
+TAIL = 2048  # last rows, compared with a call on them alone
+
+
+def test_layernorm_past_32_bits():
+    import torch
+    import paper_2605_31500_amd as gt
+    n, f = 1_100_001, 2048  # 4.5 GB a tensor
+    x, dy = rows_of_bits(n, f, 1), rows_of_bits(n, f, 2)
+    mean, rstd = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+    out = torch.empty_like(x)
+    gt.gt_layernorm_fwd(x, None, None, out, mean=mean, rstd=rstd)
+    t = slice(n - TAIL, n)
+    want, m, r = torch.empty_like(x[t]), torch.empty(TAIL, device="cuda"), torch.empty(TAIL, device="cuda")
+    gt.gt_layernorm_fwd(x[t], None, None, want, mean=m, rstd=r)
+    assert torch.equal(out[t], want) and torch.equal(mean[t], m) and torch.equal(rstd[t], r)
+    dg, db = torch.empty(f, device="cuda"), torch.empty(f, device="cuda")
+    gt.gt_layernorm_bwd(x, dy, None, mean, rstd, out, dgamma=dg, dbeta=db)
+    gt.gt_layernorm_bwd(x[t], dy[t], None, m, r, want)
+    assert torch.equal(out[t], want)
+    ref = torch.zeros(f, dtype=torch.float64, device="cuda")
+    size = torch.zeros_like(ref)
+    for a in range(0, n, 1 << 17):
+        ref += dy[a:a + (1 << 17)].double().sum(0)
+        size += dy[a:a + (1 << 17)].double().abs().sum(0)
+    # (a lane sums at most n / 256 rows in fp32, workgroups' sums are added in 64 bits)
+    assert bool(torch.all((db.double() - ref).abs() <= (n / 256 + 272) * 2.0 ** -24 * size))
+
+
+@pytest.mark.parametrize("dims,layout", [((64, 96, 96), "halves"), ((62, 90, 90), "halves")])
+def test_rope_past_32_bits(dims, layout):
+    import torch
+    import paper_2605_31500_amd as gt
+    n, h, d = 1_100_001, 8, 256
+    q = rows_of_bits(n, h * d, 3).view(n, h, d)
+    pos = torch.rand((n, 3), device="cuda") * 100
+    out = torch.empty_like(q)
+    gt.gt_rope(pos, q, out, dims, layout=layout)
+    t = slice(n - TAIL, n)
+    want = torch.empty_like(q[t])
+    gt.gt_rope(pos[t], q[t], want, dims, layout=layout)
+    assert torch.equal(out[t], want)
+    gt.gt_rope(pos, q, q, dims, layout=layout)
+    assert torch.equal(out, q)
+
+
+def test_diff_attention_past_32_bits():
+    """The last rows refer to each other: as the same graph on them alone, up to
+    the order of a row's sums (the small graph takes its rows otherwise)."""
+    import torch
+    import paper_2605_31500_amd as gt
+    n, h, d = 550_001, 8, 256  # rows of 8 KB
+    q, k, do = (rows_of_bits(n, 2 * h * d, s) for s in (5, 6, 7))
+    v = torch.flip(k, (0,))
+    rowptr, colidx = synth.ragged_graph(8, TAIL, max_deg=8, hubs={3: 300, 700: 900}, shuffle=True)
+    rt, ct = synth.transpose_csr(rowptr, colidx, TAIL)
+    lam = torch.linspace(0.1, 0.8, h, device="cuda")
+    res = []
+    for base in (0, n - TAIL):  # the tail's tensors alone, then the whole ones
+        N = TAIL if base == 0 else n
+        csr = []
+        for rp, ci in ((rowptr, colidx), (rt, ct)):
+            rp = np.concatenate([np.zeros(base, np.int64), rp])
+            csr += [to_device(rp), to_device((ci + base).astype(np.int32))]
+        t = [x[n - N:].view(N, 2 * h, d) for x in (q, k)] + [x[n - N:].view(N, h, 2 * d) for x in (v, do)]
+        out, dv = torch.empty_like(t[2]), torch.empty_like(t[2])
+        dq, dk, dl = torch.empty_like(t[0]), torch.empty_like(t[0]), torch.empty_like(lam)
+        lse = torch.empty((N, 2 * h), device="cuda")
+        gt.gt_diff_attn_fwd(csr[0], csr[1], t[0], t[1], t[2], lam, out, d ** -0.5, lse=lse)
+        gt.gt_diff_attn_bwd(*csr, t[0], t[1], t[2], lam, t[3], lse, dq, dk, dv, dl, d ** -0.5)
+        if base:
+            for x in (out, dq, dk, dv):
+                assert not torch.any(x[:base])
+            assert bool(torch.all(torch.isneginf(lse[:base])))
+        res.append([x[N - TAIL:].float().cpu().numpy() for x in (out, dq, dk, dv)] + [lse[N - TAIL:].cpu().numpy(), dl.cpu().numpy()])
+        del out, dq, dk, dv
+    for a, b in zip(*res):
+        fin = np.isfinite(a)
+        assert np.array_equal(fin, np.isfinite(b))
+        a, b = np.where(fin, a, 0), np.where(fin, b, 0)
+        # each value is rounded once to bf16, from sums that differ in fp32: by a step at most
+        assert float(np.linalg.norm(a - b)) <= 2.0 ** -7 * float(np.linalg.norm(a))
