@@ -515,8 +515,9 @@ def run_layer(args, w, gt, torch, to_device, synth) -> dict:
         "n_gpus": 1, "steps": args.steps, "warmup": args.warmup, "ms_per_step": round(ms, 5),
         "higher_is_better": True, "scaling": "weak", "vs_baseline": None, "dtype": w.dtype, "data": "synthetic",
         "config": dict(w.describe(), layer=op),
-        "roofline": {"bound": "hbm", "achieved": round(achieved, 1), "peak": HBM_PEAK_GBPS, "unit": "GB/s",
-                     "frac": round(achieved / HBM_PEAK_GBPS, 4), "algorithmic_bytes_per_launch": mbytes,
+        "roofline": {"bound": "hbm", "kernel": "whole call", "achieved": round(achieved, 1), "peak": HBM_PEAK_GBPS,
+                     "unit": "GB/s", "frac": round(achieved / HBM_PEAK_GBPS, 4),
+                     "traffic": stored_traffic("%s:%s" % (w.name, op)), "algorithmic_bytes_per_launch": mbytes,
                      "kernel_ms": round(ms, 5)},
     }
 

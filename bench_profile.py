@@ -63,6 +63,18 @@ CAPTURES = {
                    title="Segment min aggregation",
                    model="rowptr + colidx + one gathered row per entry + out + int32 sources",
                    summary="gt_reduce_kernel_{w}"),
+    "diff": dict(args=["--layer", "diff", "--config", "1"], kernels=["gt_diff_kernel"], key="{w}:diff",
+                 title="Differential attention forward", model=GT_MODEL, summary="gt_diff_kernel_{w}"),
+    "diffbwd": dict(args=["--layer", "diff-backward", "--config", "1"], kernels=["gt_diff_kernel"],
+                    key="{w}:diff-backward", passes=2, title="Differential attention backward (both passes)",
+                    model="backward per-edge model", summary="gt_diff_kernel_backward_{w}"),
+    "rope": dict(args=["--layer", "rope", "--config", "1"], kernels=["gt_rope_kernel"], key="{w}:rope",
+                 title="Rotary positions of Q and K", model="Q, K read and written once", summary="gt_rope_kernel_{w}"),
+    "norm": dict(args=["--layer", "layernorm", "--config", "1"], kernels=["gt_norm_fwd_kernel"], key="{w}:layernorm",
+                 title="Layer norm forward", model="rows read and written once", summary="gt_norm_fwd_kernel_{w}"),
+    "normbwd": dict(args=["--layer", "layernorm-backward", "--config", "1"], kernels=["gt_norm_bwd_kernel"],
+                    key="{w}:layernorm-backward", title="Layer norm backward",
+                    model="rows and their gradients read, gradients written once", summary="gt_norm_bwd_kernel_{w}"),
 }
 SQ_GROUP = ["SQ_LDS_BANK_CONFLICT", "SQ_LDS_IDX_ACTIVE", "SQ_INSTS_LDS", "SQ_INSTS_VALU", "SQ_INSTS_VMEM_RD",
             "SQ_WAVES", "GRBM_GUI_ACTIVE"]
