@@ -426,15 +426,18 @@ int norm_blocks(int64_t rows_per_block, int64_t N, int dev) {
 }
 
 template <typename T, int G, int K, int MODE>
-gt_status launch_norm(const NormArgs& a, bool backward, int dev, hipStream_t stream) {
+gt_status launch_norm_fwd(const NormArgs& a, int dev, hipStream_t stream) {
+    using Row = NormRow<T, G, K, MODE>;
+    const int blocks = norm_blocks<T, G, K, MODE, false>(Row::kGroups * Row::kAhead, a.N, dev);
+    hipLaunchKernelGGL((gt_norm_fwd_kernel<T, G, K, MODE>), dim3(blocks), dim3(Row::kThreads), 0, stream, a);
+    const hipError_t he = hipGetLastError();
+    return he == hipSuccess ? GT_SUCCESS : hip_fail(he, "layer norm launch");
+}
+
+template <typename T, int G, int K, int MODE>
+gt_status launch_norm_bwd(const NormArgs& a, int dev, hipStream_t stream) {
     using Row = NormRow<T, G, K, MODE>;
     hipError_t he = hipSuccess;
-    if (!backward) {
-        const int blocks = norm_blocks<T, G, K, MODE, false>(Row::kGroups * Row::kAhead, a.N, dev);
-        hipLaunchKernelGGL((gt_norm_fwd_kernel<T, G, K, MODE>), dim3(blocks), dim3(Row::kThreads), 0, stream, a);
-        he = hipGetLastError();
-        return he == hipSuccess ? GT_SUCCESS : hip_fail(he, "layer norm launch");
-    }
     const int blocks = norm_blocks<T, G, K, MODE, true>(Row::kGroups * Row::kAheadBwd, a.N, dev);
     CallWorkspace cw;
     if (a.dgamma || a.dbeta)
@@ -448,6 +451,11 @@ gt_status launch_norm(const NormArgs& a, bool backward, int dev, hipStream_t str
         if ((he = hipGetLastError()) != hipSuccess) return hip_fail(he, "layer norm parameter launch");
     }
     return GT_SUCCESS;
+}
+
+template <typename T, int G, int K, int MODE>
+gt_status launch_norm(const NormArgs& a, bool backward, int dev, hipStream_t stream) {
+    return backward ? launch_norm_bwd<T, G, K, MODE>(a, dev, stream) : launch_norm_fwd<T, G, K, MODE>(a, dev, stream);
 }
 
 // The lanes of a row by its accesses.  A wavefront takes rows of a few accesses
@@ -499,7 +507,7 @@ gt_status pick_phase(const NormArgs& a, bool backward, int dev, hipStream_t stre
     if (c <= 16) return launch_norm<T, 16, 1, M>(a, backward, dev, stream);
     if (c <= 32) return launch_norm<T, 32, 1, M>(a, backward, dev, stream);
     if (c <= 64) return launch_norm<T, 64, 1, M>(a, backward, dev, stream);
-    if (c <= 128 && backward) return launch_norm<T, 64, 2, M>(a, backward, dev, stream);
+    if (c <= 128 && backward) return launch_norm_bwd<T, 64, 2, M>(a, dev, stream);
     if (c <= 256) return launch_norm<T, 256, 1, M>(a, backward, dev, stream);
     if (c <= 512) return launch_norm<T, 512, 1, M>(a, backward, dev, stream);
     if (c <= 1024) return launch_norm<T, 1024, 1, M>(a, backward, dev, stream);
