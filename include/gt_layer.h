@@ -34,11 +34,11 @@ extern "C" {
  *
  * Layouts: Q, K [N][2H][D]; V, out [N][H][2D], in `dtype`, 16-byte aligned;
  * lambda float [H], any values; lse (may be NULL) float [N][2H], receives
- * ln(sum_e exp(s_m,e)).  An entry whose score is -inf has weight 0 (its
- * value row still enters, times 0); a row without entries, or with none but
- * such, counts as empty in that map: the map's sum is 0 and its lse -inf.  Inf
- * and NaN in the K or V row of a node reach only the rows whose entries name
- * that node.
+ * ln(sum_e exp(s_m,e)).  An entry whose score is -inf (or below -2.35e38: scores
+ * are held in units of ln 2) has weight 0 (its value row still enters, times 0);
+ * a row without entries, or with none but such, counts as empty in that map: the
+ * map's sum is 0 and its lse -inf.  Inf and NaN in the K or V row of a node reach
+ * only the rows whose entries name that node.
  * Supported shapes: H in {1, 2, 4, 8} with D in {32, 64, 128}, and for bf16
  * features also D = 256 (a value head's 2D elements must fit 64 lanes of 16
  * bytes); 0 <= E < 2^31; 0 <= N < 2^31.
@@ -96,9 +96,9 @@ gt_status gt_diff_attn_bwd(gt_dtype dtype, const int64_t* rowptr, const int32_t*
  *                    dims[a] / 2 pairs p after those of the axes before it
  * theta > 0, finite.  The angle is reduced to a part of a turn in 64 bits, so
  * far positions keep their accuracy; the turned values are computed in fp32 and
- * rounded once (bf16: to nearest even).  A node whose angle is not finite
- * (its position is not, or overflows) gets NaN in that axis' elements.  inverse != 0 turns by -t: the inverse, which
- * is also the operator's gradient.
+ * rounded once (bf16: to nearest even).  A node whose angle is not finite (its
+ * position is not, or it overflows) gets NaN in that axis' elements.  inverse !=
+ * 0 turns by -t: the inverse, which is also the operator's gradient.
  * Layouts: pos float [N][axes], 4-byte aligned; Q, K, outQ, outK [N][H][D] in
  * `dtype`, 16-byte aligned; K and outK may both be NULL.  outQ may be Q itself
  * and outK K itself (in place); other overlaps are refused, as are outputs that
