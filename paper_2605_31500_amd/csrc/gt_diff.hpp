@@ -55,13 +55,21 @@ struct DiffParams {
 
 // What the lanes share while a wavefront works on one slice: base pointers at
 // the slice's first element.
-template <typename T, int PS, int D>
+template <typename T, int PS, int D, bool BACKWARD>
 struct DiffSlice {
     using Gm = Geo<T, 2 * PS, D>;
     static_assert(Gm::kNV == 1, "a slice is one 16-byte vector per lane");
     static constexpr int kG = Gm::kG, kHL = Gm::kHL, kEPV = Gm::kEPV;
-    static constexpr int kU = Gm::kP >= 4 && Gm::kU >= 8 ? Gm::kU / 2 : Gm::kU;
-    static constexpr bool kSorted = Gm::kP >= 4;
+    // Entries per step: four, whose registers leave room for more wavefronts; eight in
+    // the forward where a row takes a whole wavefront (eight / four, us: R-MAT of 200 K
+    // nodes, forward bf16 1x128 424 / 389, fp32 2x64 707 / 636, fp32 1x128 699 / 730,
+    // backward 1178 / 933, 1645 / 1483, 1627 / 1607; lognormal 60 K nodes 202 / 205, 344 /
+    // 350, 389 / 400, backward 413 / 399, 716 / 726, 757 / 778).
+    static constexpr int kU = Gm::kU >= 8 && (BACKWARD || Gm::kP >= 2) ? 4 : Gm::kU;
+    // Light rows in step order where a wavefront holds two rows or more (id order / so, us:
+    // R-MAT of 200 K nodes, forward bf16 1x128 384 / 328, fp32 2x64 636 / 585, backward 930 /
+    // 779, 1486 / 1355; degree 31 throughout the same).
+    static constexpr bool kSorted = Gm::kP >= 2;
     static constexpr bool kDot2 = std::is_same<T, bf16_tag>::value;
     const char* A;
     const char* B;
@@ -127,7 +135,7 @@ template <typename T, int PS, int D>
 struct DiffFwdState;
 
 template <typename T, int PS, int D>
-struct DiffFwdOp : DiffSlice<T, PS, D> {
+struct DiffFwdOp : DiffSlice<T, PS, D, false> {
     using State = DiffFwdState<T, PS, D>;
     static constexpr int kRow = 2 * PS * D;
     static constexpr int kSlotFloats = 2 * kRow + 4 * PS;  // two accumulators, (max, sum) of each map
@@ -292,7 +300,7 @@ template <typename T, int PS, int D, int MODE>
 struct DiffBwdState;
 
 template <typename T, int PS, int D, int MODE>
-struct DiffBwdOp : DiffSlice<T, PS, D> {
+struct DiffBwdOp : DiffSlice<T, PS, D, true> {
     using State = DiffBwdState<T, PS, D, MODE>;
     static constexpr int kRow = 2 * PS * D;
     static constexpr int kSlotFloats = 2 * kRow + (MODE == 0 ? 4 * 2 * PS : 0);
